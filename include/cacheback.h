@@ -239,13 +239,82 @@ int cb_tree_attention_noalloc(const cb_config *cfg, void *hip_stream, int32_t ba
 int cb_compact_kv(cb_ctx *ctx, void *hip_stream, int32_t num_layers, const cb_kv_layer *layers,
                   int32_t *new_kv_len);
 
+/* ------------------------------------------------------------------------------------------------
+ * Around the verification: what a serving program runs on the same cache before and after it.  The tokens of one call are those
+ * of a batch of sequences back to back, sequence b's from token_offsets[b] to token_offsets[b + 1] (host [batch + 1], from 0 on, none for a
+ * sequence that has nothing new).  These calls enqueue launches only, on `hip_stream`, and can be captured into a HIP graph; kv_len and
+ * token_offsets are host arrays and travel as kernel arguments.  The context's device must be the current one.  They leave the state of the
+ * last verify call untouched, and rows behind the last sequence's tokens as they were.
+ * ------------------------------------------------------------------------------------------------ */
+
+/* What becomes of query and key heads before the attention sees them. */
+typedef struct {
+  const float *q_weight; /* device [head_dim]: x / sqrt(mean(x^2) + norm_eps) * weight for every query head; NULL = as they come */
+  const float *k_weight; /* the same for the key heads                                          */
+  const float *inv_freq; /* device [rotary_dim / 2]: radians per position; NULL when rotary_dim is 0 */
+  float norm_eps;        /* >= 0                                                                */
+  int32_t rotary_dim;    /* leading dims that are rotated: 0 or a multiple of 16 up to head_dim  */
+  int32_t interleaved;   /* pair i: 0 = dims i and i + rotary_dim / 2, 1 = dims 2 i and 2 i + 1  */
+} cb_head_prep;
+
+/*
+ * Brings new tokens into the cache: query and key heads are normalised and rotated, the queries go to q_out, keys and values to cache
+ * slots kv_len[b] + i.  One pass: everything is read and written once.  Pair (x, y) of a token at position t becomes (x cos - y sin, y cos + x sin)
+ * of t * inv_freq[pair]; the angle is reduced in 64 bits, all else is computed in 32 and rounded once, when it is stored.
+ *   q, k, v         device: token t's heads at t * q_stride ([Hq][D]), k_stride and v_stride ([Hkv][D]) elements, so that they can be
+ *                   parts of one product's rows; strides are multiples of 16 bytes.  q and q_out may both be NULL: keys and values only.
+ *   d_tree_parent   device [sumN] or NULL.  NULL: the tokens continue their sequences, token i's position is kv_len[b] + i.  Otherwise they are
+ *                   draft trees as cb_verify_tree_device takes them, of up to max_nodes nodes, and node i's position is kv_len[b] + its depth
+ *                   (malformed parents are repaired and reported as there; any depth is right).
+ *   q_out           device [sumN][Hq][D]; may be q itself where q_stride is Hq * D, else apart from q, k and v
+ * The cache must not overlap the inputs, but for a token whose k (or v) is where it goes to.  A slot whose block-table entry lies outside the
+ * pool is not written (status bit 64); two sequences whose new slots share a block leave either's rows there.
+ */
+int cb_append_kv_device(cb_ctx *ctx, void *hip_stream, int32_t batch, const void *q, int64_t q_stride,
+                        const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                        const cb_head_prep *prep, const cb_kv_layer *kv, const int32_t *kv_len,
+                        const int32_t *token_offsets, const int32_t *d_tree_parent, void *q_out);
+
+/*
+ * Attention of a chunk of new tokens over the cache: token i of sequence b attends to slots 0 .. kv_len[b] + i, whose last i + 1 hold the
+ * K/V of the chunk's own tokens (cb_append_kv_device).  For prompts, whole or in pieces of any length, and for single tokens; a batch may
+ * mix them.  max_nodes does not bound a chunk.
+ *   q, attn_out     device [sumN][Hq][D]; the softmax scale is the configuration's.  attn_out may be q.
+ * What a token must not see -- later tokens of its chunk, slots behind the sequence -- can hold anything, NaN too.
+ */
+int cb_chunk_attention_device(cb_ctx *ctx, void *hip_stream, int32_t batch, const void *q,
+                              const cb_kv_layer *kv, const int32_t *kv_len, const int32_t *token_offsets,
+                              void *attn_out);
+
+/*
+ * Log probabilities of given tokens, with each row's entropy and its likeliest tokens, from logits of the configuration's vocabulary and
+ * type, in one pass over them.  With z = log sum exp(x): log p = x - z, entropy = z - sum p x (in nats).
+ *   logits          device: row r at r * logits_stride elements (>= vocab_size; any alignment of the type), num_rows of them
+ *   n               results wanted
+ *   d_rows          device [n] or NULL: result i is for logits row d_rows[i] (the same row may be asked for more than once); NULL: for row i,
+ *                   and n <= num_rows
+ *   d_tokens        device [n] or NULL, d_logprob device [n] or NULL, both or neither: the tokens and their log probabilities
+ *   d_entropy       device [n] or NULL
+ *   d_top_tokens    device [n][top_k], the top_k largest logits' indices, largest first, the lower index first among equal ones,
+ *   d_top_logprobs  device [n][top_k], and their log probabilities; 0 <= top_k <= min(vocab_size, CB_MAX_TOP); both NULL when top_k is 0
+ * Logits may be -inf (forbidden tokens): log probability -inf, nothing to the entropy.  A row that is -inf throughout gives -inf and entropy 0;
+ * one with +inf or NaN unspecified numbers, but indices inside the vocabulary.  A result whose row lies outside [0, num_rows) has
+ * log probabilities and entropy NaN and top tokens -1; a token outside the vocabulary has log probability NaN.
+ */
+#define CB_MAX_TOP 32
+int cb_token_logprobs_device(cb_ctx *ctx, void *hip_stream, const void *logits, int64_t logits_stride,
+                             int32_t num_rows, int32_t n, const int32_t *d_rows, const int32_t *d_tokens,
+                             float *d_logprob, float *d_entropy, int32_t top_k, int32_t *d_top_tokens,
+                             float *d_top_logprobs);
+
 /* Test hooks (each synchronises the stream of the last verify call).
  *   cb_get_path     host [batch][max_depth+1]: node indices of the accepted path, -1 padded
  *   cb_get_argmax   host [sumN]: first-maximum index of each logits row
  *   cb_device_status  0, or a bit mask: 1 = malformed parent entry seen, 2 = node deeper than max_depth,
  *                     16 = (informational) a split merge had to read partials across XCDs,
  *                     32 = (informational) a workgroup of a cooperative merge gave up waiting and left
- *                     its slice to the workgroup that completed the tile */
+ *                     its slice to the workgroup that completed the tile,
+ *                     64 = cb_append_kv_device left out a slot whose block-table entry lies outside the pool */
 int cb_get_path(cb_ctx *ctx, int32_t *path);
 int cb_get_argmax(cb_ctx *ctx, int32_t *argmax);
 int cb_device_status(cb_ctx *ctx, int32_t *status);

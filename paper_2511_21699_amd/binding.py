@@ -21,7 +21,7 @@ CB_LAYOUT_TOKEN_MAJOR, CB_LAYOUT_HEAD_MAJOR = 0, 1
 ERROR_NAMES = {0: "CB_OK", 1: "CB_EINVAL", 2: "CB_ETREE", 3: "CB_ECAP", 4: "CB_ESTATE", 5: "CB_EHIP"}
 
 EXPORTS = ["cb_workspace_bytes", "cb_init", "cb_check_verify_args", "cb_plan_attention", "cb_verify_tree", "cb_verify_tree_device", "cb_verify_and_compact_device", "cb_model_step_device", "cb_tree_attention_device", "cb_tree_attention_noalloc",
-           "cb_compact_kv", "cb_get_path", "cb_get_argmax", "cb_device_status", "cb_set_option",
+           "cb_compact_kv", "cb_append_kv_device", "cb_chunk_attention_device", "cb_token_logprobs_device", "cb_get_path", "cb_get_argmax", "cb_device_status", "cb_set_option",
            "cb_last_launch_info", "cb_last_attention_ms", "cb_debug_timestamps", "cb_probe_stream_read", "cb_last_error",
            "cb_destroy"]
 
@@ -40,6 +40,11 @@ class CbConfig(C.Structure):
 class CbKvLayer(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("capacity_or_num_blocks", C.c_int64),
                 ("block_table", C.c_void_p), ("max_blocks_per_seq", C.c_int32), ("layout", C.c_int32)]
+
+
+class CbHeadPrep(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p), ("norm_eps", C.c_float),
+                ("rotary_dim", C.c_int32), ("interleaved", C.c_int32)]
 
 
 class CbError(RuntimeError):
@@ -91,6 +96,9 @@ def _prototyped(i32p):
     L.cb_tree_attention_device.argtypes = [vp, vp, C.c_int32, vp, C.POINTER(CbKvLayer), i32p, i32p, vp, vp]
     L.cb_tree_attention_noalloc.argtypes = [C.POINTER(CbConfig), vp, C.c_int32, vp, C.POINTER(CbKvLayer), i32p, i32p, vp, vp]
     L.cb_compact_kv.argtypes = [vp, vp, C.c_int32, C.POINTER(CbKvLayer), i32p]
+    L.cb_append_kv_device.argtypes = [vp, vp, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, C.POINTER(CbHeadPrep), C.POINTER(CbKvLayer), i32p, i32p, vp, vp]
+    L.cb_chunk_attention_device.argtypes = [vp, vp, C.c_int32, vp, C.POINTER(CbKvLayer), i32p, i32p, vp]
+    L.cb_token_logprobs_device.argtypes = [vp, vp, vp, C.c_int64, C.c_int32, C.c_int32, vp, vp, vp, vp, C.c_int32, vp, vp]
     L.cb_get_path.argtypes = [vp, i32p]
     L.cb_get_argmax.argtypes = [vp, i32p]
     L.cb_device_status.argtypes = [vp, i32p]
@@ -151,6 +159,23 @@ def kv_layer(k, v, block_table=None, layout: int = CB_LAYOUT_TOKEN_MAJOR, paged:
         return CbKvLayer(k.data_ptr(), v.data_ptr(), cap, block_table.data_ptr(), block_table.shape[1], layout)
     cap = k.shape[1] if layout == CB_LAYOUT_TOKEN_MAJOR else k.shape[2]
     return CbKvLayer(k.data_ptr(), v.data_ptr(), cap, None, 0, layout)
+
+
+def head_prep(q_weight=None, k_weight=None, eps: float = 1e-6, inv_freq=None, interleaved: bool = False) -> CbHeadPrep:
+    """Describe what `append_kv` does to query and key heads: fp32 tensors on the device, norm weights [head_dim] and the frequencies
+    [rotary_dim / 2] of the rotation (each may be None: not normalised, not rotated).  The descriptor keeps the tensors."""
+    p = CbHeadPrep(_f32_ptr("q_weight", q_weight), _f32_ptr("k_weight", k_weight), _f32_ptr("inv_freq", inv_freq), eps,
+                   0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0)
+    p._keep = (q_weight, k_weight, inv_freq)
+    return p
+
+
+def _f32_ptr(name, t) -> Optional[int]:
+    if t is None:
+        return None
+    if str(t.dtype) != "torch.float32" or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor")
+    return t.data_ptr()
 
 
 def check_verify_args(cfg: CbConfig, batch: int, kv: CbKvLayer, kv_len, node_offsets, parent) -> Tuple[int, str]:
@@ -325,6 +350,97 @@ class Verifier:
         marshalling would cost as much as the GPU work).  `parent` / `tokens`: int32 arrays to bind as the tree
         (a TreeGrower's outputs, say) instead of arrays of the object's own."""
         return HostStep(self, q, kv, logits, attn_out, batch, layers, stream, parent, tokens)
+
+    # ---- around the verification: tokens into the cache, their attention, their probabilities.  The `bind_` forms marshal once and return a
+    # zero-argument callable that only makes the C call; it reads the int32 arrays kv_len and token_offsets that it was given anew in every call,
+    # so a loop changes them in place.
+    def bind_append_kv(self, q, k, v, prep: CbHeadPrep, kv: CbKvLayer, kv_len, token_offsets, q_out, d_parent=None, stream=None):
+        """Pre-marshalled cb_append_kv_device.  q [n, Hq, D], k and v [n, Hkv, D] can be views of one product's rows; q and q_out may both
+        be None.  prep.q_weight and prep.k_weight must have head_dim entries."""
+        cfg = self.cfg
+        kv_len, token_offsets = _i32(kv_len), _i32(token_offsets)
+        n = self._tokens("token_offsets", token_offsets, kv_len)
+        strides = [self._heads(name, t, n, h) for name, t, h in (("q", q, cfg.num_q_heads), ("k", k, cfg.num_kv_heads), ("v", v, cfg.num_kv_heads))]
+        if q_out is not None:
+            self._heads("q_out", q_out, n, cfg.num_q_heads, True)
+        for name, w in (("q_weight", prep.q_weight), ("k_weight", prep.k_weight)):
+            t = getattr(prep, "_keep", (None, None, None))[name == "k_weight"]
+            if w and t is not None and t.numel() != cfg.head_dim:
+                raise ValueError(f"{name} must have head_dim entries")
+        if d_parent is not None and (str(d_parent.dtype) != "torch.int32" or not d_parent.is_contiguous() or d_parent.numel() < n):
+            raise ValueError("d_parent must be a contiguous int32 tensor of one entry per token")
+        at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        a = (self.ctx, self._stream(stream), len(kv_len), at(q), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2], C.byref(prep), C.byref(kv),
+             _ip(kv_len), _ip(token_offsets), at(d_parent), at(q_out))
+        return self._bound(self._F.cb_append_kv_device, a, (kv_len, token_offsets, q, k, v, prep, kv, d_parent, q_out))
+
+    def append_kv(self, q, k, v, prep: CbHeadPrep, kv: CbKvLayer, kv_len, token_offsets, q_out, d_parent=None, stream=None):
+        """Normalise and rotate new tokens' query and key heads and put their K/V into the cache (cb_append_kv_device)."""
+        self.bind_append_kv(q, k, v, prep, kv, kv_len, token_offsets, q_out, d_parent, stream)()
+
+    def bind_chunk_attention(self, q, kv: CbKvLayer, kv_len, token_offsets, attn_out, stream=None):
+        """Pre-marshalled cb_chunk_attention_device."""
+        kv_len, token_offsets = _i32(kv_len), _i32(token_offsets)
+        n = self._tokens("token_offsets", token_offsets, kv_len)
+        for name, t in (("q", q), ("attn_out", attn_out)):
+            self._heads(name, t, n, self.cfg.num_q_heads, True)
+        a = (self.ctx, self._stream(stream), len(kv_len), q.data_ptr(), C.byref(kv), _ip(kv_len), _ip(token_offsets), attn_out.data_ptr())
+        return self._bound(self._F.cb_chunk_attention_device, a, (kv_len, token_offsets, q, kv, attn_out))
+
+    def chunk_attention(self, q, kv: CbKvLayer, kv_len, token_offsets, attn_out=None, stream=None):
+        """Attention of new tokens over the cache that holds their K/V already (cb_chunk_attention_device); returns attn_out."""
+        attn_out = self._torch.empty_like(q) if attn_out is None else attn_out
+        self.bind_chunk_attention(q, kv, kv_len, token_offsets, attn_out, stream)()
+        return attn_out
+
+    def bind_token_logprobs(self, logits, d_tokens, top_k: int, logprob, entropy=None, top_tokens=None, top_logprobs=None, d_rows=None, stream=None):
+        """Pre-marshalled cb_token_logprobs_device.  logits [rows, vocab] with any row stride; d_rows: int32 row numbers, None for all rows in
+        order; d_tokens and logprob may both be None."""
+        cfg, n = self.cfg, logits.shape[0] if d_rows is None else d_rows.numel()
+        want = "torch.float32" if cfg.logits_dtype == CB_F32 else "torch.bfloat16"
+        if logits.dim() != 2 or logits.shape[1] != cfg.vocab_size or logits.stride(1) != 1 or str(logits.dtype) != want:
+            raise ValueError(f"logits must be [rows, {cfg.vocab_size}] in {want} with neighbouring entries")
+        for name, t, dt, count in (("d_rows", d_rows, "int32", n), ("d_tokens", d_tokens, "int32", n), ("logprob", logprob, "float32", n), ("entropy", entropy, "float32", n),
+                                   ("top_tokens", top_tokens, "int32", n * top_k), ("top_logprobs", top_logprobs, "float32", n * top_k)):
+            if t is not None and (str(t.dtype) != "torch." + dt or not t.is_contiguous() or t.numel() != count):
+                raise ValueError(f"{name} must be a contiguous {dt} tensor of {count} entries")
+        at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        a = (self.ctx, self._stream(stream), logits.data_ptr(), max(logits.stride(0), cfg.vocab_size) if logits.shape[0] <= 1 else logits.stride(0), logits.shape[0], n, at(d_rows),
+             at(d_tokens), at(logprob), at(entropy), top_k, at(top_tokens) if top_k else None, at(top_logprobs) if top_k else None)
+        return self._bound(self._F.cb_token_logprobs_device, a, (logits, d_rows, d_tokens, logprob, entropy, top_tokens, top_logprobs))
+
+    def token_logprobs(self, logits, d_tokens, top_k: int = 0, d_rows=None, stream=None):
+        """Log probabilities of tokens, entropies and likeliest tokens of logits rows (cb_token_logprobs_device): fresh tensors
+        (logprob [n], None without d_tokens; entropy [n], top_tokens [n, top_k], top_logprobs [n, top_k])."""
+        n = logits.shape[0] if d_rows is None else d_rows.numel()
+        f32, i32 = dict(dtype=self._torch.float32, device=logits.device), dict(dtype=self._torch.int32, device=logits.device)
+        out = (None if d_tokens is None else self._torch.empty(n, **f32), self._torch.empty(n, **f32), self._torch.empty(n, top_k, **i32), self._torch.empty(n, top_k, **f32))
+        self.bind_token_logprobs(logits, d_tokens, top_k, *out, d_rows=d_rows, stream=stream)()
+        return out
+
+    def _bound(self, fn, a, keep):
+        def call(_keep=(self, keep)):
+            rc = fn(*a)
+            if rc:
+                self._raise(rc)
+        return call
+
+    @staticmethod
+    def _tokens(name: str, offsets: np.ndarray, kv_len: np.ndarray) -> int:
+        if len(offsets) != len(kv_len) + 1:
+            raise ValueError(f"{name} must have one entry more than kv_len")
+        return int(offsets[-1])
+
+    def _heads(self, name: str, t, n: int, heads: int, contiguous: bool = False) -> int:
+        """The token stride of a [>= n, heads, head_dim] tensor of the configuration's type."""
+        if t is None and name == "q":
+            return 0
+        d, want = self.cfg.head_dim, "torch.float32" if self.cfg.qkv_dtype == CB_F32 else "torch.bfloat16"
+        if t.dim() != 3 or t.shape[0] < n or tuple(t.shape[1:]) != (heads, d) or str(t.dtype) != want or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+            raise ValueError(f"{name} must be [>= {n}, {heads}, {d}] in {want} with a token's heads side by side")
+        if contiguous and t.shape[0] > 1 and t.stride(0) != heads * d:
+            raise ValueError(f"{name} must be contiguous")
+        return max(t.stride(0), heads * d) if t.shape[0] <= 1 else t.stride(0)
 
     def compact_kv(self, layers: Sequence[CbKvLayer], batch: int, want_len: bool = True, stream=None):
         arr = C.byref(layers[0]) if len(layers) == 1 else (CbKvLayer * len(layers))(*layers)

@@ -126,6 +126,7 @@ struct Plan {
 
 struct cb_ctx {
   cb_config cfg;
+  int device;  // the one it was created on
   WsLayout lay;
   char* ws;
   // pinned host mirror
@@ -806,6 +807,20 @@ int order_behind_host_form(cb_ctx* ctx, hipStream_t st) {
   return CB_OK;
 }
 
+// After a failed launch: the kernels rely on tickets that are zero between launches.
+int clear_counters(cb_ctx* ctx, hipStream_t st, bool scans) {
+  if (!ctx->counters_dirty) return CB_OK;
+  const cb_config& c = ctx->cfg;
+  const hipError_t e1 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.tickets), ctx->lay.ticket_count / 2, 1, 1);
+  const hipError_t e2 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.coop_tickets), kCoopTiles, kCoopTicketStride / 8, 2);
+  const hipError_t e3 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.amax_tickets), c.max_batch * kTicketWords / 2, 1, 1);
+  const hipError_t e4 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.moves), (c.max_batch * c.num_kv_heads + 1) / 2, 1, 1);
+  if (e1 != hipSuccess || e2 != hipSuccess || e3 != hipSuccess || e4 != hipSuccess) return set_err(ctx, CB_EHIP, "clearing the tickets after a failed launch failed");
+  ctx->counters_dirty = false;
+  ctx->amax_dirty = ctx->amax_dirty || scans;  // (the row maxima too)
+  return CB_OK;
+}
+
 // Enqueues the whole verification on `st`; the tree is already on the device.  model: the attention of all layers of its table (q, kv and
 // attn_out are the first one's).
 int run_pipeline(cb_ctx* ctx, hipStream_t st, int batch, const void* q, const cb_kv_layer* kv,
@@ -823,15 +838,8 @@ int run_pipeline(cb_ctx* ctx, hipStream_t st, int batch, const void* q, const cb
   const int total = node_offsets[batch];
   const int ordered = order_behind_host_form(ctx, st);
   if (ordered) return ordered;
-  if (ctx->counters_dirty) {  // (after a failed launch: the kernels rely on tickets that are zero between launches)
-    const hipError_t e1 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.tickets), ctx->lay.ticket_count / 2, 1, 1);
-    const hipError_t e2 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.coop_tickets), kCoopTiles, kCoopTicketStride / 8, 2);
-    const hipError_t e3 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.amax_tickets), c.max_batch * kTicketWords / 2, 1, 1);
-    const hipError_t e4 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.moves), (c.max_batch * c.num_kv_heads + 1) / 2, 1, 1);
-    if (e1 != hipSuccess || e2 != hipSuccess || e3 != hipSuccess || e4 != hipSuccess) return set_err(ctx, CB_EHIP, "clearing the tickets after a failed launch failed");
-    ctx->counters_dirty = false;
-    ctx->amax_dirty = ctx->amax_dirty || (stage_mask & 4) != 0;  // (the row maxima too)
-  }
+  const int cleared = clear_counters(ctx, st, (stage_mask & 4) != 0);
+  if (cleared) return cleared;
   if (ctx->amax_dirty && (ctx->opt_stages & stage_mask & 12) == 12) {
     CB_HIP(ctx, launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.amax_best), ctx->lay.max_total_nodes, kAmaxStride, 1));
     ctx->amax_dirty = false;
@@ -1071,6 +1079,119 @@ bool layers_together(cb_ctx* ctx, int batch, int n, const void* const* q, const 
   return true;
 }
 
+// What the calls around the verification check of a batch: its tokens (n_max: at most so many to a sequence, 0 any number) and its
+// cache.  Fills the kernels' shapes.
+int check_tokens(cb_ctx* ctx, int32_t batch, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, int n_max, KvAddr* addr, SeqMeta* meta) {
+  const cb_config& c = ctx->cfg;
+  if (batch < 1 || batch > c.max_batch) return set_err(ctx, CB_EINVAL, "batch %d outside [1, %d]", batch, c.max_batch);
+  if (!kv->k || !kv->v || kv->capacity_or_num_blocks < 1 || (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15)) return set_err(ctx, CB_EINVAL, "bad cache descriptor");
+  if (c.block_size > 0 && (!kv->block_table || kv->max_blocks_per_seq < 1)) return set_err(ctx, CB_EINVAL, "paged cache without a block table");
+  if (!make_kv_addr(c, *kv, addr)) return set_err(ctx, CB_EINVAL, "unknown cache layout %d", kv->layout);
+  if (token_offsets[0] != 0) return set_err(ctx, CB_EINVAL, "token_offsets[0] must be 0");
+  const int64_t room = c.block_size > 0 ? (int64_t)kv->max_blocks_per_seq * c.block_size : kv->capacity_or_num_blocks;
+  for (int b = 0; b < batch; b++) {
+    const int64_t n = (int64_t)token_offsets[b + 1] - token_offsets[b];
+    if (n < 0) return set_err(ctx, CB_EINVAL, "token_offsets falls at sequence %d", b);
+    if (n_max && n > n_max) return set_err(ctx, CB_ECAP, "sequence %d has %lld nodes, max_nodes is %d", b, (long long)n, n_max);
+    if (kv_len[b] < 0) return set_err(ctx, CB_EINVAL, "negative kv_len[%d]", b);
+    if (kv_len[b] + n > room || kv_len[b] + n > (1ll << 30)) return set_err(ctx, CB_ECAP, "sequence %d does not fit the cache", b);
+    meta->kv_len[b] = kv_len[b];
+    meta->by_length[b] = b;
+  }
+  for (int b = 0; b <= CB_MAX_BATCH; b++) meta->node_off[b] = b <= batch ? token_offsets[b] : INT32_MAX;
+  return CB_OK;
+}
+
+// Before the launches of those calls: the context's device is the current one, and the stream is behind a host-form call's.
+int before_launch(cb_ctx* ctx, hipStream_t st) {
+  int device = -1;
+  CB_HIP(ctx, hipGetDevice(&device));
+  if (device != ctx->device) return set_err(ctx, CB_EINVAL, "the context is of device %d, the current one is %d", ctx->device, device);
+  return order_behind_host_form(ctx, st);
+}
+
+// The arguments of cb_append_kv_device, and what its kernel gets.
+int check_append(cb_ctx* ctx, int32_t batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                 const cb_head_prep* prep, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, const int32_t* d_tree_parent, void* q_out, AppendArgs* args, SeqMeta* meta) {
+  AppendArgs& a = *args;
+  if (!prep || !kv || !kv_len || !token_offsets) return set_err(ctx, CB_EINVAL, "null argument");
+  const cb_config& c = ctx->cfg;
+  const int rc = check_tokens(ctx, batch, kv, kv_len, token_offsets, d_tree_parent ? c.max_nodes : 0, &a.kv, meta);
+  if (rc || token_offsets[batch] == 0) return rc;  // (nothing new: there need not be tensors)
+  if (!k || !v) return set_err(ctx, CB_EINVAL, "null argument");
+  if (!q != !q_out) return set_err(ctx, CB_EINVAL, "q and q_out: both or neither");
+  if (!q) q_stride = 0;
+  const int64_t D = c.head_dim, eb = c.qkv_dtype == CB_F32 ? 4 : 2;
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out) & 15) return set_err(ctx, CB_EINVAL, "device pointers must be 16-byte aligned");
+  if ((q && q_stride < c.num_q_heads * D) || k_stride < c.num_kv_heads * D || v_stride < c.num_kv_heads * D)
+    return set_err(ctx, CB_EINVAL, "a token's stride is less than its heads");
+  if (std::max({q_stride, k_stride, v_stride}) > (1ll << 32)) return set_err(ctx, CB_EINVAL, "a token's stride is more than 2^32");
+  if (q_stride * eb % 16 || k_stride * eb % 16 || v_stride * eb % 16) return set_err(ctx, CB_EINVAL, "strides must be multiples of 16 bytes");
+  if (prep->rotary_dim < 0 || prep->rotary_dim > D || prep->rotary_dim % 16) return set_err(ctx, CB_EINVAL, "rotary_dim must be a multiple of 16 up to head_dim");
+  if (prep->rotary_dim > 0 && !prep->inv_freq) return set_err(ctx, CB_EINVAL, "rotary_dim without inv_freq");
+  if (((uintptr_t)prep->q_weight | (uintptr_t)prep->k_weight | (uintptr_t)prep->inv_freq) & 15) return set_err(ctx, CB_EINVAL, "device pointers must be 16-byte aligned");
+  if ((prep->q_weight || prep->k_weight) && !(prep->norm_eps >= 0.f)) return set_err(ctx, CB_EINVAL, "norm_eps must not be negative");
+  if (q) {
+    const size_t row = (size_t)c.num_kv_heads * D * eb, qrow = (size_t)c.num_q_heads * D * eb, last = (size_t)token_offsets[batch] - 1;
+    const Span out{q_out, (last + 1) * qrow};
+    if (!(q == q_out && q_stride == c.num_q_heads * D) && out.meets({q, last * q_stride * eb + qrow})) return set_err(ctx, CB_EINVAL, "q_out overlaps q");
+    if (out.meets({k, last * k_stride * eb + row}) || out.meets({v, last * v_stride * eb + row})) return set_err(ctx, CB_EINVAL, "q_out overlaps k or v");
+  }
+  a.q = q, a.k = k, a.v = v, a.q_out = q_out;
+  a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+  a.q_weight = prep->q_weight, a.k_weight = prep->k_weight, a.inv_freq = prep->inv_freq;
+  a.parent = d_tree_parent;
+  a.status = ctx->dev<int32_t>(ctx->lay.status);
+  a.eps = prep->norm_eps;
+  a.rotary = prep->rotary_dim, a.interleaved = prep->interleaved != 0;
+  a.Hq = c.num_q_heads, a.Hkv = c.num_kv_heads;
+  return CB_OK;
+}
+
+// The arguments of cb_chunk_attention_device, and what its kernels get.
+int check_chunk(cb_ctx* ctx, int32_t batch, const void* q, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, void* attn_out, ChunkArgs* args,
+                SeqMeta* meta) {
+  ChunkArgs& a = *args;
+  if (!kv || !kv_len || !token_offsets) return set_err(ctx, CB_EINVAL, "null argument");
+  const cb_config& c = ctx->cfg;
+  const int rc = check_tokens(ctx, batch, kv, kv_len, token_offsets, 0, &a.kv, meta);
+  a.total = rc ? 0 : token_offsets[batch];
+  if (a.total == 0) return rc;  // (nothing new: there need not be tensors)
+  if (!q || !attn_out) return set_err(ctx, CB_EINVAL, "null argument");
+  if (((uintptr_t)q | (uintptr_t)attn_out) & 15) return set_err(ctx, CB_EINVAL, "device pointers must be 16-byte aligned");
+  a.q = q;
+  a.out = attn_out;
+  a.Hq = c.num_q_heads, a.Hkv = c.num_kv_heads;
+  a.scale = c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf((float)c.head_dim);
+  const Span out{attn_out, (size_t)a.total * c.num_q_heads * c.head_dim * (c.qkv_dtype == CB_F32 ? 4 : 2)};
+  if (q != attn_out && out.meets({q, out.bytes})) return set_err(ctx, CB_EINVAL, "attn_out overlaps q and is not q");
+  return CB_OK;
+}
+
+// The arguments of cb_token_logprobs_device, and what its kernels get.
+int check_logprobs(cb_ctx* ctx, const void* logits, int64_t logits_stride, int32_t num_rows, int32_t n, const int32_t* d_rows, const int32_t* d_tokens, float* d_logprob,
+                   float* d_entropy, int32_t top_k, int32_t* d_top_tokens, float* d_top_logprobs, LogprobArgs* args) {
+  LogprobArgs& a = *args;
+  const cb_config& c = ctx->cfg;
+  if (n < 0 || num_rows < 0 || (!d_rows && n > num_rows)) return set_err(ctx, CB_EINVAL, "%d results of %d rows", n, num_rows);
+  if (n == 0) return CB_OK;  // (there need not be tensors)
+  if (!logits) return set_err(ctx, CB_EINVAL, "null argument");
+  if (!d_tokens != !d_logprob) return set_err(ctx, CB_EINVAL, "d_tokens and d_logprob: both or neither");
+  if (top_k < 0 || top_k > CB_MAX_TOP || top_k > c.vocab_size) return set_err(ctx, CB_EINVAL, "top_k %d outside [0, %d]", top_k, std::min(CB_MAX_TOP, c.vocab_size));
+  if (top_k > 0 && (!d_top_tokens || !d_top_logprobs)) return set_err(ctx, CB_EINVAL, "top_k without d_top_tokens or d_top_logprobs");
+  if (logits_stride < c.vocab_size || logits_stride > (1ll << 32)) return set_err(ctx, CB_EINVAL, "logits_stride outside [vocab_size, 2^32]");
+  const size_t lb = c.logits_dtype == CB_F32 ? 4 : 2;
+  if ((uintptr_t)logits % lb || (((uintptr_t)d_rows | (uintptr_t)d_tokens | (uintptr_t)d_logprob | (uintptr_t)d_entropy | (uintptr_t)d_top_tokens | (uintptr_t)d_top_logprobs) & 3))
+    return set_err(ctx, CB_EINVAL, "misaligned device pointer");
+  a.logits = logits;
+  a.stride = logits_stride;
+  a.rows = d_rows, a.tokens = d_tokens;
+  a.logprob = d_logprob, a.entropy = d_entropy, a.top_tokens = d_top_tokens, a.top_logprobs = d_top_logprobs;
+  a.V = c.vocab_size, a.n = n, a.num_rows = num_rows, a.top_k = top_k;
+  a.is_f32 = c.logits_dtype == CB_F32;
+  return CB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1210,6 +1331,10 @@ int cb_init(const cb_config* cfg, void* workspace, size_t workspace_bytes, cb_ct
   cb_ctx* ctx = new (std::nothrow) cb_ctx();
   if (!ctx) return set_err(nullptr, CB_EHIP, "out of host memory");
   ctx->cfg = *cfg;
+  if (const hipError_t d = hipGetDevice(&ctx->device); d != hipSuccess) {
+    delete ctx;
+    return set_err(nullptr, CB_EHIP, "hipGetDevice: %s", hipGetErrorString(d));
+  }
   ctx->lay = lay;
   ctx->ws = static_cast<char*>(workspace);
   ctx->opt_stages = 15;
@@ -1541,6 +1666,84 @@ int cb_compact_kv(cb_ctx* ctx, void* hip_stream, int32_t num_layers, const cb_kv
     }
   }
   return CB_OK;
+}
+
+int cb_append_kv_device(cb_ctx* ctx, void* hip_stream, int32_t batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                        const cb_head_prep* prep, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, const int32_t* d_tree_parent,
+                        void* q_out) {
+  if (!ctx) return set_err(nullptr, CB_EINVAL, "null context");
+  ctx->err[0] = 0;
+  AppendArgs a{};
+  SeqMeta meta{};
+  int rc = check_append(ctx, batch, q, q_stride, k, k_stride, v, v_stride, prep, kv, kv_len, token_offsets, d_tree_parent, q_out, &a, &meta);
+  if (rc || token_offsets[batch] == 0) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  rc = before_launch(ctx, st);
+  if (rc) return rc;
+  CB_HIP(ctx, launch_append(st, a, meta, ctx->cfg.qkv_dtype, ctx->cfg.head_dim, token_offsets[batch]));
+  return CB_OK;
+}
+
+int cb_chunk_attention_device(cb_ctx* ctx, void* hip_stream, int32_t batch, const void* q, const cb_kv_layer* kv, const int32_t* kv_len,
+                              const int32_t* token_offsets, void* attn_out) {
+  if (!ctx) return set_err(nullptr, CB_EINVAL, "null context");
+  ctx->err[0] = 0;
+  ChunkArgs a{};
+  SeqMeta meta{};
+  int rc = check_chunk(ctx, batch, q, kv, kv_len, token_offsets, attn_out, &a, &meta);
+  if (rc || a.total == 0) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  rc = before_launch(ctx, st);
+  if (rc) return rc;
+  CB_HIP(ctx, launch_chunk_rows(st, a, meta, ctx->cfg.qkv_dtype, ctx->cfg.head_dim));
+  return CB_OK;
+}
+
+int cb_token_logprobs_device(cb_ctx* ctx, void* hip_stream, const void* logits, int64_t logits_stride, int32_t num_rows, int32_t n, const int32_t* d_rows,
+                             const int32_t* d_tokens, float* d_logprob, float* d_entropy, int32_t top_k, int32_t* d_top_tokens, float* d_top_logprobs) {
+  if (!ctx) return set_err(nullptr, CB_EINVAL, "null context");
+  ctx->err[0] = 0;
+  LogprobArgs a{};
+  int rc = check_logprobs(ctx, logits, logits_stride, num_rows, n, d_rows, d_tokens, d_logprob, d_entropy, top_k, d_top_tokens, d_top_logprobs, &a);
+  if (rc || n == 0 || (!d_logprob && !d_entropy && top_k == 0)) return rc;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  rc = before_launch(ctx, st);
+  if (rc) return rc;
+  CB_HIP(ctx, launch_logprob(st, a));
+  return CB_OK;
+}
+
+int cb_debug_check_append(const cb_config* cfg, int32_t batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                          const cb_head_prep* prep, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, const int32_t* d_tree_parent, void* q_out,
+                          char* err) {
+  cb_ctx tmp{};
+  tmp.cfg = *cfg;
+  AppendArgs a{};
+  SeqMeta meta{};
+  const int rc = check_append(&tmp, batch, q, q_stride, k, k_stride, v, v_stride, prep, kv, kv_len, token_offsets, d_tree_parent, q_out, &a, &meta);
+  memcpy(err, tmp.err, 256);
+  return rc;
+}
+
+int cb_debug_check_chunk(const cb_config* cfg, int32_t batch, const void* q, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, void* attn_out,
+                         char* err) {
+  cb_ctx tmp{};
+  tmp.cfg = *cfg;
+  ChunkArgs a{};
+  SeqMeta meta{};
+  const int rc = check_chunk(&tmp, batch, q, kv, kv_len, token_offsets, attn_out, &a, &meta);
+  memcpy(err, tmp.err, 256);
+  return rc;
+}
+
+int cb_debug_check_logprobs(const cb_config* cfg, const void* logits, int64_t logits_stride, int32_t num_rows, int32_t n, const int32_t* d_rows, const int32_t* d_tokens,
+                            float* d_logprob, float* d_entropy, int32_t top_k, int32_t* d_top_tokens, float* d_top_logprobs, char* err) {
+  cb_ctx tmp{};
+  tmp.cfg = *cfg;
+  LogprobArgs a{};
+  const int rc = check_logprobs(&tmp, logits, logits_stride, num_rows, n, d_rows, d_tokens, d_logprob, d_entropy, top_k, d_top_tokens, d_top_logprobs, &a);
+  memcpy(err, tmp.err, 256);
+  return rc;
 }
 
 int cb_get_path(cb_ctx* ctx, int32_t* path) {

@@ -269,6 +269,42 @@ hipError_t launch_attn_wide_px(hipStream_t st, const AttnParams& p, const SeqMet
 hipError_t launch_attn_mfma(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int max_nodes_in_call,
                             int total_nodes, const LogitsWork* logits_work, const LayerTable* layers, int* merge_kind);
 
+// New tokens into the cache (cb_append.hip); strides in elements between tokens.
+struct AppendArgs {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  void* q_out;
+  KvAddr kv;
+  const float *q_weight, *k_weight, *inv_freq;
+  const int32_t* parent;  // null: the tokens continue their sequences
+  int32_t* status;
+  float eps;
+  int32_t rotary, interleaved, Hq, Hkv;
+};
+// (In the meta of launch_append and of the chunk launchers, sequences past the batch have offsets of INT_MAX.)
+hipError_t launch_append(hipStream_t st, const AppendArgs& a, const SeqMeta& meta, int dtype, int D, int total);
+
+// Attention of chunks of new tokens.
+struct ChunkArgs {
+  const void* q;  // [total][Hq][D]
+  void* out;
+  KvAddr kv;
+  int32_t Hq, Hkv, total;
+  float scale;
+};
+hipError_t launch_chunk_rows(hipStream_t st, const ChunkArgs& a, const SeqMeta& meta, int dtype, int D);
+
+// Log probabilities (cb_logprob.hip)
+struct LogprobArgs {
+  const void* logits;
+  int64_t stride;  // elements between rows
+  const int32_t *rows, *tokens;
+  float *logprob, *entropy, *top_logprobs;
+  int32_t* top_tokens;
+  int32_t V, n, num_rows, top_k, is_f32;
+};
+hipError_t launch_logprob(hipStream_t st, const LogprobArgs& a);
+
 }  // namespace cb
 
 // For tests, without a device: the plan of a verification or of the attention alone with the tallest tiles, which decides what is held in
@@ -290,3 +326,11 @@ extern "C" int cb_debug_layers(const cb_config* cfg, int32_t layers, int32_t bat
 extern "C" int cb_debug_step(cb_ctx* ctx, int32_t info[4]);
 // The pool size that the kernels clamp the block table's entries to (0: contiguous, -1: unknown layout).
 extern "C" int64_t cb_debug_pool_blocks(const cb_config* cfg, const cb_kv_layer* layer);
+// The argument checks of the calls around the verification (err: 256 bytes).
+extern "C" int cb_debug_check_append(const cb_config* cfg, int32_t batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                     int64_t v_stride, const cb_head_prep* prep, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets,
+                                     const int32_t* d_tree_parent, void* q_out, char* err);
+extern "C" int cb_debug_check_chunk(const cb_config* cfg, int32_t batch, const void* q, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets,
+                                    void* attn_out, char* err);
+extern "C" int cb_debug_check_logprobs(const cb_config* cfg, const void* logits, int64_t logits_stride, int32_t num_rows, int32_t n, const int32_t* d_rows,
+                                       const int32_t* d_tokens, float* d_logprob, float* d_entropy, int32_t top_k, int32_t* d_top_tokens, float* d_top_logprobs, char* err);
