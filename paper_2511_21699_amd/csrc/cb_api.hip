@@ -1079,6 +1079,87 @@ bool layers_together(cb_ctx* ctx, int batch, int n, const void* const* q, const 
   return true;
 }
 
+// How a chunk's attention (bf16) is cut up: tiles of so many rows, each over its keys in splits of `chunk`.
+struct ChunkPlan {
+  int tile_rows, chunk, nsplit;  // nsplit: of the longest tile
+  int64_t jobs;                  // workgroups
+  int tiles;                     // row tiles of the longest chunk, per kv head
+};
+
+// The cheapest of a few plans by an estimate of the launch's time.  A workgroup takes `start` us beside its sweep and `unit` us for every
+// 32 keys; the longest are dispatched first, so the launch ends no later than max(longest job, work / 256 compute units + the shortest job),
+// nor before the cache has been read.  Splits are for launches that leave compute units idle; their partial states have the room that
+// the workspace has.
+ChunkPlan plan_chunk(const cb_config& c, int64_t partial_room, int64_t ticket_tiles, int max_splits, int opt_splits, int opt_tile_rows, int batch, const int32_t* kv_len,
+                     const int32_t* off) {
+  const int g = c.num_q_heads / c.num_kv_heads, Hkv = c.num_kv_heads;
+  int n_max = 0, len_max = 0;
+  double slots = 0;
+  for (int b = 0; b < batch; b++) {
+    const int n = off[b + 1] - off[b];
+    if (n == 0) continue;
+    n_max = std::max(n_max, n);
+    len_max = std::max(len_max, kv_len[b] + n);
+    slots += kv_len[b] + n;
+  }
+  const double memory = slots * Hkv * c.head_dim * 4 / 5.3e6 + 3.0, by_dim = c.head_dim == 128 ? 1.0 : 0.6;
+  const int64_t m_max = (int64_t)n_max * g, one = chunk_partial_bytes(c.head_dim, off[batch], c.num_q_heads, Hkv, batch);
+  ChunkPlan best{};
+  double best_us = 0;
+  for (const int rows : {64, 128, 256}) {
+    if (best.jobs && m_max <= rows / 2) break;
+    if (opt_tile_rows && rows != opt_tile_rows && m_max > 64) continue;
+    const double unit = (rows == 256 ? 0.85 : rows == 128 ? 0.5 : 0.27) * by_dim, start = rows == 256 ? 7.0 : rows == 128 ? 5.0 : 4.0;
+    const int tiles_max = (int)((m_max + rows - 1) / rows);
+    int64_t tiles = 0;
+    for (int b = 0; b < batch; b++) tiles += ((int64_t)(off[b + 1] - off[b]) * g + rows - 1) / rows * Hkv;
+    int most = 1;
+    if (tiles <= 1024 && (int64_t)batch * Hkv * tiles_max <= ticket_tiles) {
+      const int64_t room = std::min<int64_t>(partial_room / one, ((1ll << 31) - 1) / ((int64_t)Hkv * ((m_max + 31) / 32) * (one / std::max<int64_t>(1, off[batch] * (int64_t)c.num_q_heads / 32 + (int64_t)(Hkv + 1) * batch + 1))));
+      most = (int)std::max<int64_t>(1, std::min<int64_t>({room, max_splits, (len_max + 63) / 64, 1024}));
+    }
+    int ns = opt_splits > 0 ? std::min(opt_splits, most) : 1;
+    for (int last = 0;; ns += 1 + ns / 12) {
+      ns = std::min(ns, most);
+      if (ns == last) break;
+      last = ns;
+      const int chunk = ((len_max + ns - 1) / ns + 31) / 32 * 32;
+      double work = 0, longest = 0, shortest = 1e30;
+      int64_t jobs = 0, real = 0, merged = 0;
+      for (int b = 0; b < batch; b++) {
+        const int n = off[b + 1] - off[b], s = kv_len[b], nt = (int)(((int64_t)n * g + rows - 1) / rows);
+        if (n == 0) continue;
+        jobs += (int64_t)nt * Hkv * ((s + n + chunk - 1) / chunk);
+        if (ns == 1) {  // (whole tiles: their lengths are evenly spaced)
+          const double first = start + unit * ((s + std::min(n, (rows + g - 1) / g) + 31) / 32), end = start + unit * ((s + n + 31) / 32);
+          work += 0.5 * (first + end) * nt * Hkv;
+          longest = std::max(longest, end);
+          shortest = std::min(shortest, first);
+          real += (int64_t)nt * Hkv;
+          continue;
+        }
+        for (int t = 0; t < nt; t++) {
+          const int len = s + (int)((std::min<int64_t>((int64_t)(t + 1) * rows, (int64_t)n * g) - 1) / g) + 1, full = len / chunk, rest = len - full * chunk;
+          const double f = start + unit * (chunk / 32), r = rest ? start + unit * ((rest + 31) / 32) : 1e30;
+          work += (full * f + (rest ? r : 0.0)) * Hkv;
+          longest = std::max(longest, full ? f : r);
+          shortest = std::min(shortest, std::min(full ? f : 1e30, r));
+          real += (int64_t)(full + (rest > 0)) * Hkv;
+          merged += (full + (rest > 0)) > 1 ? Hkv : 0;
+        }
+      }
+      const double merge = ns == 1 ? 0.0 : real <= 256 ? 1.5 : 2.0 + 0.4 * ns * (rows / 128.0);
+      const double us = std::max(memory + (ns > 1 ? merge : 0.0), real <= 256 ? longest + merge : std::max(longest + merge, (work + merged * merge) / 256 + shortest));
+      if (best.jobs == 0 || us < best_us - 0.2) {
+        best = ChunkPlan{rows, chunk, (len_max + chunk - 1) / chunk, jobs, tiles_max};
+        best_us = us;
+      }
+      if (opt_splits > 0) break;
+    }
+  }
+  return best;
+}
+
 // What the calls around the verification check of a batch: its tokens (n_max: at most so many to a sequence, 0 any number) and its
 // cache.  Fills the kernels' shapes.
 int check_tokens(cb_ctx* ctx, int32_t batch, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, int n_max, KvAddr* addr, SeqMeta* meta) {
@@ -1695,7 +1776,43 @@ int cb_chunk_attention_device(cb_ctx* ctx, void* hip_stream, int32_t batch, cons
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   rc = before_launch(ctx, st);
   if (rc) return rc;
-  CB_HIP(ctx, launch_chunk_rows(st, a, meta, ctx->cfg.qkv_dtype, ctx->cfg.head_dim));
+  const cb_config& c = ctx->cfg;
+  if (c.qkv_dtype == CB_F32 || (c.block_size & (c.block_size - 1)) || ctx->opt_impl == 1) {
+    CB_HIP(ctx, launch_chunk_rows(st, a, meta, c.qkv_dtype, c.head_dim));
+    return CB_OK;
+  }
+  rc = clear_counters(ctx, st, true);
+  if (rc) return rc;
+  const ChunkPlan plan = plan_chunk(c, ctx->lay.total - ctx->lay.partial, ctx->lay.ticket_count / 4, ctx->lay.max_splits, (int)ctx->opt_splits, (int)ctx->opt_tile_rows, batch,
+                                    kv_len, token_offsets);
+  if (plan.jobs > INT32_MAX) return set_err(ctx, CB_EINVAL, "too many tokens in one call");
+  auto len = [&](int b) { return token_offsets[b + 1] == token_offsets[b] ? 0 : kv_len[b] + token_offsets[b + 1] - token_offsets[b]; };
+  std::stable_sort(meta.by_length, meta.by_length + batch, [&](int32_t x, int32_t y) { return len(x) > len(y); });
+  int64_t before = 0;
+  for (int i = 0; i < CB_MAX_BATCH; i++) {
+    meta.start[i] = i < batch && before < plan.jobs ? (int32_t)before : INT32_MAX;
+    if (i >= batch) continue;
+    const int b = meta.by_length[i];
+    const int64_t rows = (int64_t)(token_offsets[b + 1] - token_offsets[b]) * (c.num_q_heads / c.num_kv_heads);
+    before += (rows + plan.tile_rows - 1) / plan.tile_rows * c.num_kv_heads * ((len(b) + plan.chunk - 1) / plan.chunk);
+  }
+  AttnParams p{};
+  p.q = q;
+  p.out = attn_out;
+  p.kv = a.kv;
+  p.partial = ctx->dev<float>(ctx->lay.partial);
+  p.tickets = ctx->dev<uint32_t>(ctx->lay.tickets);
+  p.coop_tickets = ctx->dev<uint32_t>(ctx->lay.coop_tickets);
+  p.Hq = c.num_q_heads, p.Hkv = c.num_kv_heads, p.D = c.head_dim;
+  p.chunk = plan.chunk, p.nsplit = plan.nsplit, p.tile_rows = plan.tile_rows;
+  p.batch = batch;
+  p.scale = a.scale;
+  p.grid_y = plan.tiles;
+  p.spin_limit = (int32_t)ctx->opt_spin;
+  p.status = ctx->dev<int32_t>(ctx->lay.status);
+  // (the whole launch resident at once, a workgroup to a compute unit: see split_merge)
+  p.coop_merge = ctx->opt_coop && plan.nsplit > 1 && plan.nsplit <= 64 && plan.jobs <= 256 && (int64_t)batch * c.num_kv_heads * plan.tiles <= kCoopTiles;
+  CB_LAUNCH(ctx, launch_attn_chunk(st, p, meta, (int)plan.jobs));
   return CB_OK;
 }
 

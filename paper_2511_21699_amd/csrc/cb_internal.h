@@ -293,6 +293,10 @@ struct ChunkArgs {
   float scale;
 };
 hipError_t launch_chunk_rows(hipStream_t st, const ChunkArgs& a, const SeqMeta& meta, int dtype, int D);
+// bf16 on the matrix cores, blocks of a power of two (cb_attn_chunk.hip): grid_y = row tiles of the longest chunk per kv head, meta.start =
+// workgroups in front of each sequence's, in the order of meta.by_length
+hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs);
+int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch);  // of one split
 
 // Log probabilities (cb_logprob.hip)
 struct LogprobArgs {
