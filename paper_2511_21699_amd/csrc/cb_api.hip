@@ -31,7 +31,7 @@ size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct WsLayout {
   size_t anc, parent, tokens, amax_best, amax_out, path, len_ctx, res_len, res_tok, new_len, status,
-      tickets, coop_tickets, amax_tickets, moves, dbg, partial, total;
+      tickets, coop_tickets, amax_tickets, moves, lp_tickets, dbg, lp_partial, partial, total;
   int amax_chunks;
   int max_total_nodes;
   int max_splits;
@@ -90,7 +90,9 @@ WsLayout ws_layout(const cb_config& c) {
   L.amax_tickets = take((size_t)c.max_batch * kTicketWords * 4);
   L.amax_best = take(mt * kAmaxStride * 8);
   L.moves = take((size_t)c.max_batch * c.num_kv_heads * 4);
+  L.lp_tickets = take((size_t)kLpWgs / 2 * kLpTicketStride * 4);
   L.dbg = take(1024 * 8 * 8);
+  L.lp_partial = take((size_t)kLpWgs * (kLpHeader + CB_MAX_TOP) * 8);
   // The scalar kernel's fp32 partials are twice the size of the MFMA kernel's.  A configuration
   // the MFMA kernel takes (bf16) runs the scalar one only on request (option
   // "attn_impl" = 1, a test aid) or when its geometry is not the MFMA kernel's (see Planner::cut): it gets
@@ -815,7 +817,8 @@ int clear_counters(cb_ctx* ctx, hipStream_t st, bool scans) {
   const hipError_t e2 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.coop_tickets), kCoopTiles, kCoopTicketStride / 8, 2);
   const hipError_t e3 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.amax_tickets), c.max_batch * kTicketWords / 2, 1, 1);
   const hipError_t e4 = launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.moves), (c.max_batch * c.num_kv_heads + 1) / 2, 1, 1);
-  if (e1 != hipSuccess || e2 != hipSuccess || e3 != hipSuccess || e4 != hipSuccess) return set_err(ctx, CB_EHIP, "clearing the tickets after a failed launch failed");
+  const hipError_t e5 = ctx->lay.lp_tickets ? launch_zero_words(st, ctx->dev<unsigned long long>(ctx->lay.lp_tickets), kLpWgs / 2 * kLpTicketStride / 2, 1, 1) : hipSuccess;
+  if (e1 != hipSuccess || e2 != hipSuccess || e3 != hipSuccess || e4 != hipSuccess || e5 != hipSuccess) return set_err(ctx, CB_EHIP, "clearing the tickets after a failed launch failed");
   ctx->counters_dirty = false;
   ctx->amax_dirty = ctx->amax_dirty || scans;  // (the row maxima too)
   return CB_OK;
@@ -1826,7 +1829,11 @@ int cb_token_logprobs_device(cb_ctx* ctx, void* hip_stream, const void* logits, 
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   rc = before_launch(ctx, st);
   if (rc) return rc;
-  CB_HIP(ctx, launch_logprob(st, a));
+  rc = clear_counters(ctx, st, true);
+  if (rc) return rc;
+  a.partial = ctx->dev<unsigned long long>(ctx->lay.lp_partial);
+  a.tickets = ctx->dev<uint32_t>(ctx->lay.lp_tickets);
+  CB_LAUNCH(ctx, launch_logprob(st, a));
   return CB_OK;
 }
 

@@ -298,14 +298,22 @@ hipError_t launch_chunk_rows(hipStream_t st, const ChunkArgs& a, const SeqMeta& 
 hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs);
 int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch);  // of one split
 
-// Log probabilities (cb_logprob.hip)
+// Log probabilities (cb_logprob.hip).  The parts of a row, where there are several: a state of kLpHeader + top_k 64-bit words each in the
+// workspace, and a ticket for the row.
+constexpr int kLpParts = 16;         // at most
+constexpr int kLpWgs = 256;          // at most, where rows have parts
+constexpr int kLpHeader = 2;
+constexpr int kLpTicketStride = 16;  // 32-bit words between tickets (64 bytes)
 struct LogprobArgs {
   const void* logits;
   int64_t stride;  // elements between rows
   const int32_t *rows, *tokens;
   float *logprob, *entropy, *top_logprobs;
   int32_t* top_tokens;
+  unsigned long long* partial;  // [kLpWgs][kLpHeader + CB_MAX_TOP]
+  uint32_t* tickets;            // [kLpWgs / 2], zero between launches
   int32_t V, n, num_rows, top_k, is_f32;
+  int32_t parts;  // of a row (the launcher's)
 };
 hipError_t launch_logprob(hipStream_t st, const LogprobArgs& a);
 
