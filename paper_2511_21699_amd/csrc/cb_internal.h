@@ -300,7 +300,7 @@ int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch);  
 
 // Log probabilities (cb_logprob.hip).  The parts of a row, where there are several: a state of kLpHeader + top_k 64-bit words each in the
 // workspace, and a ticket for the row.
-constexpr int kLpParts = 16;         // at most
+constexpr int kLpParts = 8;          // at most
 constexpr int kLpWgs = 256;          // at most, where rows have parts
 constexpr int kLpHeader = 2;
 constexpr int kLpTicketStride = 16;  // 32-bit words between tickets (64 bytes)
