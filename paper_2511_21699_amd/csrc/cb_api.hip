@@ -1082,7 +1082,7 @@ bool layers_together(cb_ctx* ctx, int batch, int n, const void* const* q, const 
   return true;
 }
 
-// How a chunk's attention (bf16) is cut up: tiles of so many rows, each over its keys in splits of `chunk`.
+// How a chunk's attention is cut up: tiles of so many rows, each over its keys in splits of `chunk`.
 struct ChunkPlan {
   int tile_rows, chunk, nsplit;  // nsplit: of the longest tile
   int64_t jobs;                  // workgroups
@@ -1093,8 +1093,8 @@ struct ChunkPlan {
 // 32 keys; the longest are dispatched first, so the launch ends no later than max(longest job, work / 256 compute units + the shortest job),
 // nor before the cache has been read.  Splits are for launches that leave compute units idle; their partial states have the room that
 // the workspace has.
-ChunkPlan plan_chunk(const cb_config& c, int64_t partial_room, int64_t ticket_tiles, int max_splits, int opt_splits, int opt_tile_rows, int batch, const int32_t* kv_len,
-                     const int32_t* off) {
+ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, int opt_tile_rows, int batch, const int32_t* kv_len, const int32_t* off) {
+  const bool f32 = c.qkv_dtype == CB_F32;
   const int g = c.num_q_heads / c.num_kv_heads, Hkv = c.num_kv_heads;
   int n_max = 0, len_max = 0;
   double slots = 0;
@@ -1105,22 +1105,31 @@ ChunkPlan plan_chunk(const cb_config& c, int64_t partial_room, int64_t ticket_ti
     len_max = std::max(len_max, kv_len[b] + n);
     slots += kv_len[b] + n;
   }
-  const double memory = slots * Hkv * c.head_dim * 4 / 5.3e6 + 3.0, by_dim = c.head_dim == 128 ? 1.0 : 0.6;
-  const int64_t m_max = (int64_t)n_max * g, one = chunk_partial_bytes(c.head_dim, off[batch], c.num_q_heads, Hkv, batch);
+  const double memory = slots * Hkv * c.head_dim * (f32 ? 8 : 4) / 5.3e6 + 3.0, by_dim = c.head_dim == 128 ? 1.0 : 0.6;
+  const int64_t m_max = (int64_t)n_max * g, total = off[batch];
+  // A split's partial states, and tiles that there are tickets for.  (Within a sequence the bf16 kernel's offsets have 31 bits.)
+  const int64_t per_split = f32 ? total * c.num_q_heads * partial_stride(c.head_dim) * 4 : chunk_partial_bytes(c.head_dim, total, c.num_q_heads, Hkv, batch);
+  const int64_t tickets = f32 ? lay.ticket_count : lay.ticket_count / 4;
+  const int64_t most_here = f32 ? INT32_MAX : ((1ll << 31) - 1) / chunk_partial_bytes(c.head_dim, n_max, c.num_q_heads, Hkv, 2);
+  struct Tile {
+    int rows;
+    double unit, start;
+  };
+  static const Tile kBf16[] = {{64, 0.27, 4.0}, {128, 0.5, 5.0}, {256, 0.85, 7.0}}, kF32[] = {{16, 0.43, 3.0}, {32, 0.8, 4.0}};
   ChunkPlan best{};
   double best_us = 0;
-  for (const int rows : {64, 128, 256}) {
+  for (int kind = 0; kind < (f32 ? 2 : 3); kind++) {
+    const Tile& tile = f32 ? kF32[kind] : kBf16[kind];
+    const int rows = tile.rows;
     if (best.jobs && m_max <= rows / 2) break;
-    if (opt_tile_rows && rows != opt_tile_rows && m_max > 64) continue;
-    const double unit = (rows == 256 ? 0.85 : rows == 128 ? 0.5 : 0.27) * by_dim, start = rows == 256 ? 7.0 : rows == 128 ? 5.0 : 4.0;
+    if (!f32 && opt_tile_rows && rows != opt_tile_rows && m_max > 64) continue;
+    const double unit = tile.unit * by_dim, start = tile.start;
     const int tiles_max = (int)((m_max + rows - 1) / rows);
     int64_t tiles = 0;
     for (int b = 0; b < batch; b++) tiles += ((int64_t)(off[b + 1] - off[b]) * g + rows - 1) / rows * Hkv;
     int most = 1;
-    if (tiles <= 1024 && (int64_t)batch * Hkv * tiles_max <= ticket_tiles) {
-      const int64_t room = std::min<int64_t>(partial_room / one, ((1ll << 31) - 1) / ((int64_t)Hkv * ((m_max + 31) / 32) * (one / std::max<int64_t>(1, off[batch] * (int64_t)c.num_q_heads / 32 + (int64_t)(Hkv + 1) * batch + 1))));
-      most = (int)std::max<int64_t>(1, std::min<int64_t>({room, max_splits, (len_max + 63) / 64, 1024}));
-    }
+    if (tiles <= 1024 && (int64_t)batch * Hkv * tiles_max <= tickets)
+      most = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(lay.total - lay.partial) / per_split, most_here, lay.max_splits, (len_max + 63) / 64, 1024}));
     int ns = opt_splits > 0 ? std::min(opt_splits, most) : 1;
     for (int last = 0;; ns += 1 + ns / 12) {
       ns = std::min(ns, most);
@@ -1780,14 +1789,14 @@ int cb_chunk_attention_device(cb_ctx* ctx, void* hip_stream, int32_t batch, cons
   rc = before_launch(ctx, st);
   if (rc) return rc;
   const cb_config& c = ctx->cfg;
-  if (c.qkv_dtype == CB_F32 || (c.block_size & (c.block_size - 1)) || ctx->opt_impl == 1) {
+  const bool f32 = c.qkv_dtype == CB_F32;
+  if ((!f32 && (c.block_size & (c.block_size - 1))) || ctx->opt_impl == 1) {
     CB_HIP(ctx, launch_chunk_rows(st, a, meta, c.qkv_dtype, c.head_dim));
     return CB_OK;
   }
   rc = clear_counters(ctx, st, true);
   if (rc) return rc;
-  const ChunkPlan plan = plan_chunk(c, ctx->lay.total - ctx->lay.partial, ctx->lay.ticket_count / 4, ctx->lay.max_splits, (int)ctx->opt_splits, (int)ctx->opt_tile_rows, batch,
-                                    kv_len, token_offsets);
+  const ChunkPlan plan = plan_chunk(c, ctx->lay, (int)ctx->opt_splits, (int)ctx->opt_tile_rows, batch, kv_len, token_offsets);
   if (plan.jobs > INT32_MAX) return set_err(ctx, CB_EINVAL, "too many tokens in one call");
   auto len = [&](int b) { return token_offsets[b + 1] == token_offsets[b] ? 0 : kv_len[b] + token_offsets[b + 1] - token_offsets[b]; };
   std::stable_sort(meta.by_length, meta.by_length + batch, [&](int32_t x, int32_t y) { return len(x) > len(y); });
@@ -1815,7 +1824,7 @@ int cb_chunk_attention_device(cb_ctx* ctx, void* hip_stream, int32_t batch, cons
   p.status = ctx->dev<int32_t>(ctx->lay.status);
   // (the whole launch resident at once, a workgroup to a compute unit: see split_merge)
   p.coop_merge = ctx->opt_coop && plan.nsplit > 1 && plan.nsplit <= 64 && plan.jobs <= 256 && (int64_t)batch * c.num_kv_heads * plan.tiles <= kCoopTiles;
-  CB_LAUNCH(ctx, launch_attn_chunk(st, p, meta, (int)plan.jobs));
+  CB_LAUNCH(ctx, f32 ? launch_attn_chunk_f32(st, p, meta, (int)plan.jobs) : launch_attn_chunk(st, p, meta, (int)plan.jobs));
   return CB_OK;
 }
 

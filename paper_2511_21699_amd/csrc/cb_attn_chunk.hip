@@ -7,6 +7,7 @@
 // Probabilities are rounded to bf16, the matrix cores' type (half a step each, in the numerator and, the same, in the denominator); sums,
 // statistics and partial states are in 32 bits.
 #include "cb_attn_wide.h"
+#include "cb_chunk.h"
 
 namespace cb {
 
@@ -321,34 +322,6 @@ __device__ __forceinline__ void sweep_chunk(const AttnParams& p, const TileJob& 
     }
     write_rows<D, 32, true, PP>(p, jb, rw * R + t, grow[t], f, kw * PP, mfin, lsum, c2, kw == 0, l);
   }
-}
-
-// The workgroup's (tile, split).  Workgroups are numbered sequence by sequence, the longest first, a sequence's tiles from the last, whose
-// sweep is the longest, to the first, then splits, and the kv head runs fastest: what is dispatched last is short, and with a
-// multiple of 8 kv heads a head's tiles share an XCD's L2.
-__device__ __forceinline__ bool chunk_job(const AttnParams& p, const SeqMetaLanes& ml, int d, TileJob& j) {
-  const int i = __popcll(__builtin_amdgcn_ballot_w64(ml.start <= d)) - 1;  // (starts past the batch are INT_MAX)
-  j.b = __builtin_amdgcn_readlane(ml.ord, i);
-  const int at = d - __builtin_amdgcn_readlane(ml.start, i);
-  const SeqShape s = seq_shape(ml, j.b);
-  j.g = p.Hq / p.Hkv;
-  j.hk = at % p.Hkv;
-  j.M = s.N * j.g;
-  const int rest = at / p.Hkv, splits = (s.S + s.N + p.chunk - 1) / p.chunk, tiles = (j.M + p.tile_rows - 1) / p.tile_rows;
-  j.split = rest % splits;
-  j.rt = tiles - 1 - rest / splits;
-  j.tiles = p.grid_y;
-  j.off = s.off;
-  j.N = s.N;
-  j.S = s.S;
-  j.layer = 0;
-  j.row0 = j.rt * p.tile_rows;
-  const int last = (j.row0 + p.tile_rows < j.M ? j.row0 + p.tile_rows : j.M) - 1, len = s.S + last / j.g + 1;
-  j.k0 = j.split * p.chunk;
-  if (j.k0 >= len) return false;
-  j.k1 = j.k0 + p.chunk < len ? j.k0 + p.chunk : len;
-  j.nsplit = (len + p.chunk - 1) / p.chunk;
-  return true;
 }
 
 template <int D, bool PG>

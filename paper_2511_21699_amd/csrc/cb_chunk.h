@@ -1,0 +1,35 @@
+// What the kernels of a chunk's attention share (cb_attn_chunk.hip, cb_attn_chunk_f32.hip).  gfx950 only.
+#pragma once
+#include "cb_attn_tile.h"
+
+namespace cb {
+
+// The workgroup's (tile, split).  Workgroups are numbered sequence by sequence, the longest first, a sequence's tiles from the last, whose
+// sweep is the longest, to the first, then splits, and the kv head runs fastest: what is dispatched last is short, and with a
+// multiple of 8 kv heads a head's tiles share an XCD's L2.
+__device__ __forceinline__ bool chunk_job(const AttnParams& p, const SeqMetaLanes& ml, int d, TileJob& j) {
+  const int i = __popcll(__builtin_amdgcn_ballot_w64(ml.start <= d)) - 1;  // (starts past the batch are INT_MAX)
+  j.b = __builtin_amdgcn_readlane(ml.ord, i);
+  const int at = d - __builtin_amdgcn_readlane(ml.start, i);
+  const SeqShape s = seq_shape(ml, j.b);
+  j.g = p.Hq / p.Hkv;
+  j.hk = at % p.Hkv;
+  j.M = s.N * j.g;
+  const int rest = at / p.Hkv, splits = (s.S + s.N + p.chunk - 1) / p.chunk, tiles = (j.M + p.tile_rows - 1) / p.tile_rows;
+  j.split = rest % splits;
+  j.rt = tiles - 1 - rest / splits;
+  j.tiles = p.grid_y;
+  j.off = s.off;
+  j.N = s.N;
+  j.S = s.S;
+  j.layer = 0;
+  j.row0 = j.rt * p.tile_rows;
+  const int last = (j.row0 + p.tile_rows < j.M ? j.row0 + p.tile_rows : j.M) - 1, len = s.S + last / j.g + 1;
+  j.k0 = j.split * p.chunk;
+  if (j.k0 >= len) return false;
+  j.k1 = j.k0 + p.chunk < len ? j.k0 + p.chunk : len;
+  j.nsplit = (len + p.chunk - 1) / p.chunk;
+  return true;
+}
+
+}  // namespace cb

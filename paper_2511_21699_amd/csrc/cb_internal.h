@@ -296,6 +296,7 @@ hipError_t launch_chunk_rows(hipStream_t st, const ChunkArgs& a, const SeqMeta& 
 // bf16 on the matrix cores, blocks of a power of two (cb_attn_chunk.hip): grid_y = row tiles of the longest chunk per kv head, meta.start =
 // workgroups in front of each sequence's, in the order of meta.by_length
 hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs);
+hipError_t launch_attn_chunk_f32(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs);
 int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch);  // of one split
 
 // Log probabilities (cb_logprob.hip).  The parts of a row, where there are several: a state of kLpHeader + top_k 64-bit words each in the
