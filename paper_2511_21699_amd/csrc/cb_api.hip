@@ -1115,14 +1115,14 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     int rows;
     double unit, start;
   };
-  static const Tile kBf16[] = {{64, 0.27, 4.0}, {128, 0.5, 5.0}, {256, 0.85, 7.0}}, kF32[] = {{16, 0.43, 3.0}, {32, 0.8, 4.0}};
+  static const Tile kBf16[] = {{64, 0.38, 5.0}, {128, 0.4, 4.0}}, kF32[] = {{16, 0.43, 3.0}, {32, 0.8, 4.0}};
   ChunkPlan best{};
   double best_us = 0;
-  for (int kind = 0; kind < (f32 ? 2 : 3); kind++) {
+  for (int kind = 0; kind < 2; kind++) {
     const Tile& tile = f32 ? kF32[kind] : kBf16[kind];
     const int rows = tile.rows;
     if (best.jobs && m_max <= rows / 2) break;
-    if (!f32 && opt_tile_rows && rows != opt_tile_rows && m_max > 64) continue;
+    if (!f32 && opt_tile_rows && rows != std::min(opt_tile_rows, 128) && m_max > 64) continue;
     const double unit = tile.unit * by_dim, start = tile.start;
     const int tiles_max = (int)((m_max + rows - 1) / rows);
     int64_t tiles = 0;

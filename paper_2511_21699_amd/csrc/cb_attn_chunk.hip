@@ -18,9 +18,16 @@ __device__ __forceinline__ void mask_chunk(floatx16& s, int key0, int seen, int 
   for (int v = 0; v < 16; v++) s[v] = 8 * (v >> 2) + (v & 3) < n ? s[v] : -INFINITY;
 }
 
-// A value that a query must not see reaches its sum with weight 0, which hides it only if it is finite.  So units that some
-// query of the tile does not see whole are added up with 0 in the place of infinities and NaN, and these, which hardly ever are there,
-// separately to the queries that do see them.
+// A value that a query must not see reaches its sum with weight 0, which hides it only if it is finite; and the denominator's MFMA has the
+// probabilities of two queries in a column, one of them times 0.  So where some query does not see a unit whole, infinities and NaN
+// among its values, and queries whose largest score is one, are looked out for, and a tile that has any is swept again with care: with 0 in
+// the place of infinities and NaN, and these added up separately for the queries that do see them.
+__device__ __forceinline__ uint32_t odd_bits(const uintx4& x, uint32_t bits) {  // (an exponent of ones overflows into the sign's place: bits 15 and 31)
+#pragma unroll
+  for (int i = 0; i < 4; i++) bits |= (x[i] & 0x7f807f80u) + 0x00800080u;
+  return bits;
+}
+
 __device__ __forceinline__ bf16x8 finite_only(bf16x8 a, bool& odd) {
   uintx4 x = __builtin_bit_cast(uintx4, a);
 #pragma unroll
@@ -31,17 +38,19 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 a, bool& odd) {
   }
   return __builtin_bit_cast(bf16x8, x);
 }
+// p0, p1: the lane's probabilities (B operands); v_at: the unit's values in LDS.
 template <int D>
-__device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16x8& p0, const bf16x8& p1, uint32_t v_at, CB_LDS uint16_t* scratch, int l) {
+__device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16x8& p0, const bf16x8& p1, uint32_t v_at, int l) {
   const int r = l & 31, h = l >> 5;
-#pragma unroll
-  for (int e = 0; e < 8; e++) {
-    scratch[(8 * (e >> 2) + 4 * h + (e & 3)) * 32 + r] = __builtin_bit_cast(uint16_t, (__bf16)p0[e]);
-    scratch[(16 + 8 * (e >> 2) + 4 * h + (e & 3)) * 32 + r] = __builtin_bit_cast(uint16_t, (__bf16)p1[e]);
-  }
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  const uintx4 x0 = __builtin_bit_cast(uintx4, p0), x1 = __builtin_bit_cast(uintx4, p1);
   for (int kk = 0; kk < kUnitKeys; kk++) {
-    const float pk = __uint_as_float((uint32_t)scratch[kk * 32 + r] << 16);
+    // key 16 j + 8 (e / 4) + 4 h + e % 4 is element e of operand j of the lane in half h
+    const int at = (kk >> 4) * 4 + (kk >> 3 & 1) * 2 + (kk >> 1 & 1);
+    uint32_t pair = x0[0];
+#pragma unroll
+    for (int i = 1; i < 8; i++) pair = at == i ? (i < 4 ? x0[i & 3] : x1[i & 3]) : pair;
+    pair = (uint32_t)__shfl((int)pair, (kk >> 2 & 1) * 32 + r, 64);
+    const float pk = __uint_as_float(kk & 1 ? pair & 0xffff0000u : pair << 16);
 #pragma unroll
     for (int dt = 0; dt < D / 32; dt++)
 #pragma unroll
@@ -54,14 +63,13 @@ __device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16
 }
 
 // The sweep of one workgroup whose tile has RW row groups of R row tiles each, up to its output rows (a single split) or its
-// partial state.
-template <int D, bool PG, int R, int RW>
-__device__ __forceinline__ void sweep_chunk(const AttnParams& p, const TileJob& jb, TileLds& sh, uint4* ring) {
+// partial state.  Without CARE it returns true where the tile has to be swept with.
+template <int D, bool PG, int R, int RW, bool CARE>
+__device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& jb, TileLds& sh, uint4* ring) {
   using Part = PartialLayout<D, 32, true>;
   using F = Feed<D, kWideWaves, 32>;
   constexpr int KW = kWideWaves / RW;    // key groups
   constexpr int NS = F::kSlots, PRO = F::kPrologue;
-  constexpr int NPB = 2;                 // B operands of a unit's probabilities
   // (scores run one stage ahead of the softmax: two stages are resident while a third is requested)
   static_assert(3 * KW <= NS && KW <= PRO, "a stage is requested in full while the one before it is worked on");
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
@@ -126,16 +134,10 @@ __device__ __forceinline__ void sweep_chunk(const AttnParams& p, const TileJob& 
     if (more > 0) feed.request_units(more);
     if (nu < NS - 2) wait_vmcnt<0>();
   };
-  auto top = [&] {  // of a stage in the general loop, whose last reads may still be under way
-    wait_vmcnt<F::kReq * (NS - 6)>();
-    ring_barrier();
-    feed.request_units(KW);
-  };
-  // this wave's stages whose units are all prefix and all inside the split (rounds down; may be negative: none)
-  auto fast_stages = [&] {
-    const int n = ((S < k1 ? S : k1) - k0 - kw * kUnitKeys) / (kUnitKeys * KW);
-    return nst < n ? nst : n;
-  };
+  // whether some query may not see some key of the stage, or the split ends in it (uniform in the workgroup)
+  const int whole_end = S < k1 ? S : k1;
+  const bool hides = S < k1;  // (not for single tokens)
+  auto masked = [&](int s) { return k0 + (s + 1) * KW * kUnitKeys > whole_end; };
   // Places in the ring, in bytes, of this wave's units of the current stage and the two behind it
   constexpr uint32_t kSlotBytes = F::kSlotBytes;
   auto next_place = [&](uint32_t x) { return x + KW * kSlotBytes >= NS * kSlotBytes ? x + KW * kSlotBytes - NS * kSlotBytes : x + KW * kSlotBytes; };
@@ -149,46 +151,21 @@ __device__ __forceinline__ void sweep_chunk(const AttnParams& p, const TileJob& 
   const uint32_t lane_v = (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + kSlotBytes / 2 + lane_v_byte<D>(l);
   const bf16x8 ones = half_ones(l);
 
-  auto unit_scores = [&](int s, uint32_t place, floatx16 (&sc)[R]) {
-    uint4 k[D / 16];
-    read_k<D>(lane_k + place, k);
-    scores<D, R>(k, st, sc);
-    const int key0 = k0 + (s * KW + kw) * kUnitKeys;
-    if (key0 + kUnitKeys > S || key0 + kUnitKeys > k1)
+  uint32_t odd = 0;  // bits 15 and 31: infinities or NaN
+  auto look = [&](int s) {  // the stage's values, this wavefront's share
+    if (!hides || !masked(s)) return;
+    constexpr uint32_t kShare = kSlotBytes / 2 * KW / kWideWaves;
+    const uint32_t from = (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + at + kSlotBytes / 2 + rw * kShare + l * 16;
 #pragma unroll
-      for (int t = 0; t < R; t++) mask_chunk(sc[t], key0, seen[t], k1, h);
+    for (uint32_t x = 0; x < kShare; x += 1024) odd = odd_bits(__builtin_bit_cast(uintx4, *(const CB_LDS uintx4*)(from + x)), odd);
   };
-  auto add_unit = [&](int s, const bf16x8 (&pb)[R][NPB], uint32_t place) {
-    const uint32_t va = lane_v + place;
-    const bool careful = k0 + (s * KW + kw) * kUnitKeys + kUnitKeys > S;  // (uniform)
-    bool odd = false, odd_p = false;
-    // (the denominator's MFMA has the probabilities of two queries in a column, one of them times 0)
+  auto mask = [&](int s, floatx16 (&sc)[R]) {
+    if (!masked(s)) return;
 #pragma unroll
-    for (int t = 0; t < R; t++)
-#pragma unroll
-      for (int j = 0; j < NPB; j++)
-        st[t].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, careful ? finite_only(pb[t][j], odd_p) : pb[t][j], st[t].lacc, 0, 0, 0);
-#pragma unroll
-    for (int j = 0; j < 2; j++)
-#pragma unroll
-      for (int dt = 0; dt < D / 32; dt++) {
-        bf16x8 a = read_v<D>(va, dt, j);
-        if (careful) a = finite_only(a, odd);
-#pragma unroll
-        for (int t = 0; t < R; t++)
-#pragma unroll
-          for (int x = j; x < NPB; x += 2) st[t].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t][x], st[t].o[dt], 0, 0, 0);
-      }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
-      static_assert(sizeof(sh.anc) >= kWideWaves * kUnitKeys * 32 * 2, "");
-#pragma unroll
-      for (int t = 0; t < R; t++)
-        add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + place + kSlotBytes / 2, (CB_LDS uint16_t*)&sh.anc + w * (kUnitKeys * 32), l);
-    }
+    for (int t = 0; t < R; t++) mask_chunk(sc[t], k0 + (s * KW + kw) * kUnitKeys, seen[t], k1, h);
   };
   auto sweep = [&] {
     floatx16 sc[R];
-    bf16x8 pb[R][NPB];
     float mx[R];
     auto check = [&] {
       bool raise = mx[0] > st[0].top;  // (false for NaN)
@@ -198,23 +175,29 @@ __device__ __forceinline__ void sweep_chunk(const AttnParams& p, const TileJob& 
         for (int t = 0; t < R; t++) raise_reference<D>(st[t], mx[t], c2);
       }
     };
-    auto maxima = [&](const floatx16 (&x)[R]) {
-#pragma unroll
-      for (int t = 0; t < R; t++) mx[t] = row_max(x[t]);
-    };
-    unit_scores(0, at, sc);
-    maxima(sc);
-    check();
-    int s = 0;
-    const int fast_end = fast_stages();
     floatx16 sd[R];
     uint4 k[D / 16];
-    uintx4 pw[R][NPB];
+    uintx4 pw[R][2];
     bf16x8 v[D / 32];
-    // Stages whose units are all prefix, two at a time (the scores alternate between two sets of registers), the requests
-    // spread over the steps (all at once they hold up the wave that makes them).  One barrier per two units.
-    auto step = [&](const floatx16 (&from)[R], floatx16 (&to)[R], bool barrier) {  // stage s; from: its scores, to: those of stage s + 1
+    read_k<D>(lane_k + at, k);
+    scores<D, R>(k, st, sc);
+    mask(0, sc);
+#pragma unroll
+    for (int t = 0; t < R; t++) mx[t] = row_max(sc[t]);
+    auto odd_max = [&](int s) {
+      if (!hides || !masked(s)) return;
+#pragma unroll
+      for (int t = 0; t < R; t++) odd |= mx[t] < INFINITY ? 0u : 0x8000u;
+    };
+    odd_max(0);
+    check();
+    int s = 0;
+    // A step: the scores of stage s + 1 beside the exponentials of stage s, then its values; two at a time (the scores alternate between two
+    // sets of registers), the requests spread over the steps (all at once they hold up the wave that makes them).  With one key group
+    // a barrier for two steps.
+    auto step = [&](const floatx16 (&from)[R], floatx16 (&to)[R], bool barrier, bool masks) {  // from: the scores of stage s, to: those of stage s + 1
       if (barrier) ready();
+      if (masks) look(s);
       int64_t off[KW][F::kParts];
       uint32_t dst[KW];
 #pragma unroll
@@ -223,54 +206,132 @@ __device__ __forceinline__ void sweep_chunk(const AttnParams& p, const TileJob& 
       score_half<D, false, R, KW * F::kReq>(k, st, from, to, pw, lane_v + at, v, c2, [&](int i) {
         feed.request(i % F::kReq, off[i / F::kReq], dst[i / F::kReq]);
       });
+      if (masks) mask(s + 1, to);
       add_half<D, false, R, KW == 1>(k, lane_k + at2, lane_v + at, v, st, pw, to, mx, ones);
+      if (masks) odd_max(s + 1);
       check();
       advance();
       s++;
     };
     first_ready();
-    if (s + 2 < fast_end) {
-      if (KW == 1) {  // (K operands are a step ahead in registers)
-        ready();
-        read_k<D>(lane_k + at1, k);
-      }
-      do {
-        step(sc, sd, true);
-        step(sd, sc, KW > 1);
-      } while (s + 2 < fast_end);
+    if (nst > 1 && KW == 1) {  // (K operands are a step ahead in registers)
+      ready();
+      read_k<D>(lane_k + at1, k);
     }
-    for (; s + 1 < nst; s++) {
-      top();
-      floatx16 sn[R];
-      unit_scores(s + 1, at1, sn);
-#pragma unroll
-      for (int t = 0; t < R; t++) probs<D, false>(sc[t], st[t], c2, pb[t]);
-      add_unit(s, pb, at);
-      maxima(sn);
-      check();
-#pragma unroll
-      for (int t = 0; t < R; t++) sc[t] = sn[t];
-      advance();
+    while (s + 2 < nst && !masked(s + 2)) {
+      step(sc, sd, true, false);
+      step(sd, sc, KW > 1, false);
     }
+    bf16x8 pb[R][2];
+    auto add_unit = [&] {
+      const uint32_t va = lane_v + at;
+#pragma unroll
+      for (int t = 0; t < R; t++)
+#pragma unroll
+        for (int j = 0; j < 2; j++) st[t].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[t][j], st[t].lacc, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; dt++) {
+          const bf16x8 a = read_v<D>(va, dt, j);
+#pragma unroll
+          for (int t = 0; t < R; t++) st[t].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t][j], st[t].o[dt], 0, 0, 0);
+        }
+    };
+    // Stages with masks, one at a time.
+    while (s + 1 < nst) {
+      const bool barrier = KW > 1 || (s & 1) == 0;
+      step(sc, sd, barrier, true);
+#pragma unroll
+      for (int t = 0; t < R; t++) sc[t] = sd[t];
+    }
+    look(s);
 #pragma unroll
     for (int t = 0; t < R; t++) probs<D, false>(sc[t], st[t], c2, pb[t]);
-    add_unit(s, pb, at);
+    add_unit();
   };
-  if (has_rows) sweep();
-  else {  // no rows of its own: it only brings its share, passing the same barriers
-    int s = 0;
+  // The same with care, a stage at a time.
+  auto careful_sweep = [&] {
+    auto top = [&] {  // (the stage's last reads may still be under way)
+      wait_vmcnt<F::kReq * (NS - 6)>();
+      ring_barrier();
+      feed.request_units(KW);
+    };
     first_ready();
-    if constexpr (KW == 1) {
-      const int fast_end = fast_stages();
-      if (s + 2 < fast_end) ready();
-      for (; s + 2 < fast_end; s += 2) {
-        ready();
-        feed.request_units(2);
+    if (!has_rows) {
+      for (int s = 0; s + 1 < nst; s++) top();
+      return;
+    }
+    floatx16 sc[R];
+    bf16x8 pb[R][2];
+    for (int s = 0; s < nst; s++) {
+      if (s > 0) {
+        advance();
+        top();
+      }
+      uint4 k[D / 16];
+      read_k<D>(lane_k + at, k);
+      scores<D, R>(k, st, sc);
+      mask(s, sc);
+      bool raise = false, odd_v = false, odd_p = false;
+      float mx[R];
+#pragma unroll
+      for (int t = 0; t < R; t++) {
+        mx[t] = row_max(sc[t]);
+        raise |= mx[t] > st[t].top;
+      }
+      if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+#pragma unroll
+        for (int t = 0; t < R; t++) raise_reference<D>(st[t], mx[t], c2);
+      }
+#pragma unroll
+      for (int t = 0; t < R; t++) {
+        probs<D, false>(sc[t], st[t], c2, pb[t]);
+#pragma unroll
+        for (int j = 0; j < 2; j++) st[t].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, finite_only(pb[t][j], odd_p), st[t].lacc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; dt++) {
+          const bf16x8 a = finite_only(read_v<D>(lane_v + at, dt, j), odd_v);
+#pragma unroll
+          for (int t = 0; t < R; t++) st[t].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t][j], st[t].o[dt], 0, 0, 0);
+        }
+      if (__builtin_amdgcn_ballot_w64(odd_v) != 0) {
+#pragma unroll
+        for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + at + kSlotBytes / 2, l);
       }
     }
-    for (; s + 1 < nst; s++) top();
+  };
+  if constexpr (CARE) careful_sweep();
+  else if (has_rows) sweep();
+  else {  // no rows of its own: it only brings its share, passing the same barriers
+    first_ready();
+    if (nst > 1 && KW == 1) ready();
+    int s = 0;
+    auto step = [&](bool barrier) {
+      if (barrier) ready();
+      look(s);
+      feed.request_units(KW);
+      advance();
+      s++;
+    };
+    while (s + 2 < nst) {
+      step(true);
+      step(KW > 1);
+    }
+    if (s + 1 < nst) step(true);
+    look(s);
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
+  if (!CARE && hides) {
+    if (tid == 0) sh.flag = 0;
+    __syncthreads();
+    if (__builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0) != 0 && l == 0) sh.flag = 1;
+    __syncthreads();
+    if (sh.flag) return true;
+  }
   // With two key groups each finishes one half of the pieces: all park their accumulators and (mref, l) in the
   // ring, then each adds up the groups' for its own pieces.
   constexpr int P = Part::P, PP = P / KW;
@@ -322,10 +383,278 @@ __device__ __forceinline__ void sweep_chunk(const AttnParams& p, const TileJob& 
     }
     write_rows<D, 32, true, PP>(p, jb, rw * R + t, grow[t], f, kw * PP, mfin, lsum, c2, kw == 0, l);
   }
+  return false;
+}
+
+// Tiles of up to 128 rows, four wavefronts of 32 rows, two workgroups to a compute unit: the one's start, tail and barriers are behind the
+// other's sweep.  K and V have rings of their own, a unit's K being read a step before its V, so that 72 KiB hold the unit that is
+// worked on and three that are under way.
+template <int D>
+struct ManyLds {
+  static constexpr int kK = 4, kV = 5;                          // units
+  static constexpr int kBytes = kUnitKeys * D * 2;              // of a unit's K, or V
+  uint4 ring[(kK + kV) * kBytes / 16];
+  int bt[kBtLds];
+  int flag;
+};
+
+template <int D, bool PG>
+struct ManyFeed {
+  using F = Feed<D, kWideWaves, 32>;
+  using L = ManyLds<D>;
+  static constexpr int P = F::kParts, RPR = F::RPR;
+  static_assert(F::kReq == 2 * P, "a group is a request for K and one for V");
+  F& f;
+  int key[P];                            // the lane's row in the next unit's groups, at most the split's last key
+  const int last;
+  const CB_GLOBAL char *kb[P], *vb[P];   // what the row's offset is added to
+  uint32_t k_place = 0, v_place = 0;     // of the next unit in the rings, bytes
+  int blk[P];                            // paged: the rows' entries of the block table
+  __device__ __forceinline__ explicit ManyFeed(F& feed) : f(feed), last(feed.jb.k1 - 1) {
+    const AttnParams& p = f.p;
+    const int lr = f.l / F::VPR, lc = f.l % F::VPR;
+    const int64_t head = ((PG ? 0 : (int64_t)f.jb.b * p.kv.seq_stride) + (int64_t)f.jb.hk * p.kv.head_stride) * 2;
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+      const int rr = f.part_row(i) + lr;
+      key[i] = f.jb.k0 + rr;
+      key[i] = key[i] < last ? key[i] : last;
+      kb[i] = f.kbase + head + (lc ^ swizzle_k<D>(rr)) * 16;
+      vb[i] = f.vbase + head + (lc ^ swizzle_v<D, 32>(rr)) * 16;
+      blk[i] = 0;
+    }
+    if (PG) look_up();
+  }
+  __device__ __forceinline__ void look_up() {
+#pragma unroll
+    for (int i = 0; i < P; i++) blk[i] = f.bt[((key[i] >> f.ka.bs_shift) - f.ka.bt_first) & (kBtLds - 1)];
+  }
+  // The next unit's addresses, and on to the one behind it (whose table entries are asked for here and looked at a step later).
+  __device__ __forceinline__ void next(int64_t (&off)[P], uint32_t& kd, uint32_t& vd) {
+    const KvAddr& a = f.p.kv;
+    if (PG) {
+      if (f.long_slice) f.bt_ahead(f.requested);
+#pragma unroll
+      for (int i = 0; i < P; i++) {
+        int b = blk[i];
+        b = b < 0 ? 0 : (b >= (int)a.num_blocks ? (int)a.num_blocks - 1 : b);
+        off[i] = (int64_t)(uint64_t)(uint32_t)b * (a.seq_stride * 2) + (int64_t)((uint64_t)(uint32_t)(key[i] & (a.block_size - 1)) * (uint32_t)f.ts2);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; i++) off[i] = (int64_t)((uint64_t)(uint32_t)key[i] * (uint32_t)f.ts2);
+    }
+#pragma unroll
+    for (int i = 0; i < P; i++) {
+      key[i] += kUnitKeys;
+      key[i] = key[i] < last ? key[i] : last;
+    }
+    if (PG) look_up();
+    const uint32_t at = f.part_row(0) * (2 * D) + __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(CB_LDS uint4*)f.ring);
+    kd = at + k_place;
+    vd = at + v_place + L::kK * L::kBytes;
+    k_place = k_place + L::kBytes == L::kK * L::kBytes ? 0 : k_place + L::kBytes;
+    v_place = v_place + L::kBytes == L::kV * L::kBytes ? 0 : v_place + L::kBytes;
+    f.requested++;
+  }
+  // request i of a unit's 2 P (a constant): the groups' K, then their V
+  __device__ __forceinline__ void request(int i, const int64_t (&off)[P], uint32_t kd, uint32_t vd) const {
+    const int part = i % P;
+    lds_dma_b128_at((i < P ? kb[part] : vb[part]) + off[part], (i < P ? kd : vd) + part * (RPR * 2 * D));
+  }
+  __device__ __forceinline__ void request_unit() {
+    int64_t off[P];
+    uint32_t kd, vd;
+    next(off, kd, vd);
+#pragma unroll
+    for (int i = 0; i < 2 * P; i++) request(i, off, kd, vd);
+  }
+};
+
+// Up to the tile's output rows or its partial state.  Without CARE it returns true where the tile has to be swept with.
+template <int D, bool PG, bool CARE>
+__device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& jb, ManyLds<D>& sh) {
+  using Part = PartialLayout<D, 32, true>;
+  using F = Feed<D, kWideWaves, 32>;
+  using L = ManyLds<D>;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, r = l & 31, h = l >> 5;
+  const CB_GLOBAL uint16_t* gq = (const CB_GLOBAL uint16_t*)p.q;
+  const int S = jb.S + jb.row0 / jb.g + 1;  // (every row sees the keys below)
+  const int k0 = jb.k0, k1 = jb.k1;
+  F ring_feed(p, jb, sh.bt, sh.ring);
+  ManyFeed<D, PG> feed(ring_feed);
+  TileState<D> st[1];
+  int row = jb.row0 + w * 32 + r;
+  const bool valid = row < jb.M;
+  row = valid ? row : jb.M - 1;
+  const int token = row / jb.g, seen = jb.S + token + 1;
+  const int64_t gr = (int64_t)(jb.off + token) * p.Hq + jb.hk * jb.g + (row - token * jb.g), grow = valid ? gr : -1;
+  const CB_GLOBAL uintx4* qp = (const CB_GLOBAL uintx4*)(gq + gr * D);
+#pragma unroll
+  for (int ds = 0; ds < D / 16; ds++) st[0].q[ds] = __builtin_bit_cast(bf16x8, load_b128_untracked(qp + 2 * ds + h));
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+    for (int v = 0; v < 16; v++) st[0].o[dt][v] = 0.f;
+  st[0].lacc = floatx4{0.f, 0.f, 0.f, 0.f};
+  st[0].mref = st[0].top = -INFINITY;
+  st[0].nm = 0.f;
+  const bool has_rows = jb.row0 + w * 32 < jb.M;
+  const float c2 = p.scale * 1.4426950408889634f;  // softmax scale in the log2 domain
+  const int nst = (k1 - k0 + kUnitKeys - 1) / kUnitKeys;
+  for (int u = 0; u < L::kK; u++) feed.request_unit();  // (past the split's end: its last key)
+  wait_vmcnt<F::kReq * L::kK - F::kReq / 2>();
+  ring_barrier();
+#pragma unroll
+  for (int ds = 0; ds < D / 16; ds++) asm volatile("" : "+v"(st[0].q[ds]));  // (older than every unit)
+  // At the barrier of step s units up to s + 3 have been requested, and K up to s + 1 and V up to s have landed; everybody is done with K(s) and
+  // V(s - 1), whose places take those of unit s + 4.
+  auto ready = [&] {
+    wait_vmcnt<F::kReq / 2 + 2 * F::kReq>();
+    bare_barrier();
+  };
+  auto last_ready = [&] {  // (the last unit's V)
+    wait_vmcnt<3 * F::kReq>();
+    bare_barrier();
+  };
+  const int whole_end = S < k1 ? S : k1;
+  const bool hides = S < k1;  // (not for single tokens)
+  auto masked = [&](int s) { return k0 + (s + 1) * kUnitKeys > whole_end; };
+  const uint32_t ring = (uint32_t)(uintptr_t)(CB_LDS uint4*)sh.ring, vring = ring + L::kK * L::kBytes;
+  const uint32_t lane_k = ring + lane_k_byte<D>(l), lane_v = vring + lane_v_byte<D>(l);
+  const bf16x8 ones = half_ones(l);
+  uint32_t k_at = 0, v_at = 0;  // places of K(s + 1) and V(s); K's is that of K(0) at first
+  auto advance_k = [&] { k_at = k_at + L::kBytes == L::kK * L::kBytes ? 0 : k_at + L::kBytes; };
+  auto advance_v = [&] { v_at = v_at + L::kBytes == L::kV * L::kBytes ? 0 : v_at + L::kBytes; };
+  uint32_t odd = 0;  // bits 15 and 31: infinities or NaN
+  auto look = [&](int s) {  // the unit's values, this wavefront's share
+    if (!hides || !masked(s)) return;
+    constexpr uint32_t kShare = L::kBytes / kWideWaves;
+#pragma unroll
+    for (uint32_t x = 0; x < kShare; x += 1024) odd = odd_bits(__builtin_bit_cast(uintx4, *(const CB_LDS uintx4*)(vring + v_at + w * kShare + x + l * 16)), odd);
+    asm volatile("" : "+v"(odd));  // (the reads are through before the next barrier)
+  };
+  auto mask = [&](int s, floatx16 (&sc)[1]) {
+    if (masked(s)) mask_chunk(sc[0], k0 + s * kUnitKeys, seen, k1, h);
+  };
+  auto raise = [&](float mx) {  // (false for NaN)
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > st[0].top) != 0, 0)) raise_reference<D>(st[0], mx, c2);
+  };
+  auto sweep = [&] {
+    floatx16 sc[1], sd[1];
+    float mx[1];
+    uint4 k[D / 16];
+    uintx4 pw[1][2];
+    bf16x8 v[D / 32];
+    auto odd_max = [&](int s) {
+      if (hides && masked(s)) odd |= mx[0] < INFINITY ? 0u : 0x8000u;
+    };
+    read_k<D>(lane_k, k);
+    scores<D, 1>(k, st, sc);
+    mask(0, sc);
+    mx[0] = row_max(sc[0]);
+    odd_max(0);
+    raise(mx[0]);
+    advance_k();
+    // A step: the scores of unit s + 1 beside the exponentials of unit s, then its values.
+    auto step = [&](int s, const floatx16 (&from)[1], floatx16 (&to)[1], bool masks) {  // from: the scores of unit s, to: those of unit s + 1
+      ready();
+      read_k<D>(lane_k + k_at, k);
+      if (masks) look(s);
+      int64_t off[F::kParts];
+      uint32_t kd, vd;
+      feed.next(off, kd, vd);
+      score_half<D, false, 1, F::kReq>(k, st, from, to, pw, lane_v + v_at, v, c2, [&](int i) { feed.request(i, off, kd, vd); });
+      if (masks) mask(s + 1, to);
+      add_half<D, false, 1, false>(k, 0, lane_v + v_at, v, st, pw, to, mx, ones);
+      if (masks) odd_max(s + 1);
+      raise(mx[0]);
+      advance_k();
+      advance_v();
+    };
+    int s = 0;
+    for (; s + 2 < nst && !masked(s + 2); s += 2) {  // (the scores alternate between two sets of registers)
+      step(s, sc, sd, false);
+      step(s + 1, sd, sc, false);
+    }
+    for (; s + 1 < nst; s++) {
+      step(s, sc, sd, true);
+      sc[0] = sd[0];
+    }
+    last_ready();
+    look(s);
+    bf16x8 pb[2];
+    probs<D, false>(sc[0], st[0], c2, pb);
+#pragma unroll
+    for (int j = 0; j < 2; j++) st[0].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[j], st[0].lacc, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++) st[0].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v<D>(lane_v + v_at, dt, j), pb[j], st[0].o[dt], 0, 0, 0);
+  };
+  auto careful_sweep = [&] {  // a unit at a time
+    if (has_rows)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++) asm volatile("" : "+v"(st[0].o[dt]));
+    for (int s = 0; s < nst; s++) {
+      wait_vmcnt<0>();
+      ring_barrier();
+      if (s > 0) feed.request_unit();
+      if (has_rows) {
+        uint4 k[D / 16];
+        floatx16 sc[1];
+        bf16x8 pb[2];
+        bool odd_v = false, odd_p = false;
+        read_k<D>(lane_k + k_at, k);
+        scores<D, 1>(k, st, sc);
+        mask(s, sc);
+        raise(row_max(sc[0]));
+        probs<D, false>(sc[0], st[0], c2, pb);
+#pragma unroll
+        for (int j = 0; j < 2; j++) st[0].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, finite_only(pb[j], odd_p), st[0].lacc, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 2; j++)
+#pragma unroll
+          for (int dt = 0; dt < D / 32; dt++)
+            st[0].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_only(read_v<D>(lane_v + v_at, dt, j), odd_v), pb[j], st[0].o[dt], 0, 0, 0);
+        if (__builtin_amdgcn_ballot_w64(odd_v) != 0) add_odd_values<D>(st[0].o, pb[0], pb[1], vring + v_at, l);
+      }
+      advance_k();
+      advance_v();
+    }
+  };
+  if constexpr (CARE) careful_sweep();
+  else if (has_rows) sweep();
+  else {  // no rows of its own: it only brings its share, passing the same barriers
+    for (int s = 0; s + 1 < nst; s++) {
+      ready();
+      look(s);
+      feed.request_unit();
+      advance_v();
+    }
+    last_ready();
+    look(nst - 1);
+  }
+  wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
+  if (!CARE && hides) {
+    if (tid == 0) sh.flag = 0;
+    __syncthreads();
+    if (__builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0) != 0 && l == 0) sh.flag = 1;
+    __syncthreads();
+    if (sh.flag) return true;
+  }
+  floatx4 f[Part::P];
+#pragma unroll
+  for (int pc = 0; pc < Part::P; pc++) {
+    const floatx16& o = st[0].o[pc >> 2];
+    f[pc] = floatx4{o[4 * (pc & 3)], o[4 * (pc & 3) + 1], o[4 * (pc & 3) + 2], o[4 * (pc & 3) + 3]};
+  }
+  write_rows<D, 32, true, Part::P>(p, jb, w, grow, f, 0, st[0].mref, st[0].lacc[0], c2, true, l);
+  return false;
 }
 
 template <int D, bool PG>
-__global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk(AttnParams p_arg, SeqMeta meta) {
+__global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_few(AttnParams p_arg, SeqMeta meta) {
   const SeqMetaLanes ml = seq_meta_prefetch(meta);
   __shared__ __align__(1024) uint4 ring[Feed<D, kWideWaves, 32>::kRingVecs];
   __shared__ TileLds sh;
@@ -333,11 +662,23 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk(AttnParams p_arg, 
   pin_args(p);
   TileJob jb;
   if (!chunk_job(p, ml, blockIdx.x, jb)) return;
-  const int rows = jb.M - jb.row0 < p.tile_rows ? jb.M - jb.row0 : p.tile_rows;
-  if (rows <= 64) sweep_chunk<D, PG, 1, 2>(p, jb, sh, ring);
-  else if (rows <= 128) sweep_chunk<D, PG, 1, 4>(p, jb, sh, ring);
-  else sweep_chunk<D, PG, 2, 4>(p, jb, sh, ring);
-  if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 256, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
+  if (sweep_chunk<D, PG, 1, 2, false>(p, jb, sh, ring)) sweep_chunk<D, PG, 1, 2, true>(p, jb, sh, ring);
+  if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
+}
+
+template <int D, bool PG>
+__global__ __launch_bounds__(64 * kWideWaves, 2) void k_chunk_many(AttnParams p_arg, SeqMeta meta) {
+  const SeqMetaLanes ml = seq_meta_prefetch(meta);
+  __shared__ __align__(1024) ManyLds<D> sh;
+  AttnParams p = p_arg;
+  pin_args(p);
+  TileJob jb;
+  if (!chunk_job(p, ml, blockIdx.x, jb)) return;
+  if (sweep_many<D, PG, false>(p, jb, sh)) sweep_many<D, PG, true>(p, jb, sh);
+  if (jb.nsplit == 1) return;
+  __syncthreads();  // (everybody is done with the rings, whose place the merge's words take)
+  static_assert(sizeof(TileLds) <= sizeof(sh.ring), "");
+  split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, *reinterpret_cast<TileLds*>(sh.ring), nullptr, [] {});
 }
 
 int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch) {
@@ -345,14 +686,18 @@ int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch) {
   return tiles * (D == 64 ? PartialLayout<64, 32, true>::kBytes : PartialLayout<128, 32, true>::kBytes);
 }
 
-hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs) {
+template <int D>
+static hipError_t launch_dim(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs) {
   const dim3 grid(wgs), block(64 * kWideWaves);
   const bool paged = p.kv.block_size > 0;
-  if (p.D == 64 && paged) hipLaunchKernelGGL((k_chunk<64, true>), grid, block, 0, st, p, meta);
-  else if (p.D == 64) hipLaunchKernelGGL((k_chunk<64, false>), grid, block, 0, st, p, meta);
-  else if (paged) hipLaunchKernelGGL((k_chunk<128, true>), grid, block, 0, st, p, meta);
-  else hipLaunchKernelGGL((k_chunk<128, false>), grid, block, 0, st, p, meta);
+  if (p.tile_rows == 64 && paged) hipLaunchKernelGGL((k_chunk_few<D, true>), grid, block, 0, st, p, meta);
+  else if (p.tile_rows == 64) hipLaunchKernelGGL((k_chunk_few<D, false>), grid, block, 0, st, p, meta);
+  else if (paged) hipLaunchKernelGGL((k_chunk_many<D, true>), grid, block, 0, st, p, meta);
+  else hipLaunchKernelGGL((k_chunk_many<D, false>), grid, block, 0, st, p, meta);
   return hipGetLastError();
+}
+hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs) {
+  return p.D == 64 ? launch_dim<64>(st, p, meta, wgs) : launch_dim<128>(st, p, meta, wgs);
 }
 
 }  // namespace cb
