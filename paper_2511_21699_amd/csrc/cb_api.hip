@@ -1115,14 +1115,14 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     int rows;
     double unit, start;
   };
-  static const Tile kBf16[] = {{64, 0.38, 5.0}, {128, 0.4, 4.0}}, kF32[] = {{16, 0.43, 3.0}, {32, 0.8, 4.0}};
+  static const Tile kBf16[] = {{64, 0.38, 5.0}, {128, 0.5, 4.0}, {256, 0.95, 6.0}}, kF32[] = {{16, 0.43, 3.0}, {32, 0.8, 4.0}};
   ChunkPlan best{};
   double best_us = 0;
-  for (int kind = 0; kind < 2; kind++) {
+  for (int kind = 0; kind < (f32 ? 2 : 3); kind++) {
     const Tile& tile = f32 ? kF32[kind] : kBf16[kind];
     const int rows = tile.rows;
     if (best.jobs && m_max <= rows / 2) break;
-    if (!f32 && opt_tile_rows && rows != std::min(opt_tile_rows, 128) && m_max > 64) continue;
+    if (!f32 && opt_tile_rows && rows != opt_tile_rows && m_max > 64) continue;
     const double unit = tile.unit * by_dim, start = tile.start;
     const int tiles_max = (int)((m_max + rows - 1) / rows);
     int64_t tiles = 0;
@@ -1819,6 +1819,7 @@ int cb_chunk_attention_device(cb_ctx* ctx, void* hip_stream, int32_t batch, cons
   p.chunk = plan.chunk, p.nsplit = plan.nsplit, p.tile_rows = plan.tile_rows;
   p.batch = batch;
   p.scale = a.scale;
+  p.grid_x = (int32_t)plan.jobs;
   p.grid_y = plan.tiles;
   p.spin_limit = (int32_t)ctx->opt_spin;
   p.status = ctx->dev<int32_t>(ctx->lay.status);
@@ -1856,6 +1857,17 @@ int cb_debug_check_append(const cb_config* cfg, int32_t batch, const void* q, in
   const int rc = check_append(&tmp, batch, q, q_stride, k, k_stride, v, v_stride, prep, kv, kv_len, token_offsets, d_tree_parent, q_out, &a, &meta);
   memcpy(err, tmp.err, 256);
   return rc;
+}
+
+int cb_debug_chunk_plan(const cb_config* cfg, int32_t batch, const int32_t* kv_len, const int32_t* token_offsets, int32_t splits, int32_t tile_rows, int32_t plan[5]) {
+  if (!config_ok(cfg, nullptr, 0)) return CB_EINVAL;
+  const ChunkPlan p = plan_chunk(*cfg, ws_layout(*cfg), splits, tile_rows, batch, kv_len, token_offsets);
+  plan[0] = p.tile_rows;
+  plan[1] = p.nsplit;
+  plan[2] = p.chunk;
+  plan[3] = (int32_t)std::min<int64_t>(p.jobs, INT32_MAX);
+  plan[4] = p.tiles;
+  return CB_OK;
 }
 
 int cb_debug_check_chunk(const cb_config* cfg, int32_t batch, const void* q, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, void* attn_out,

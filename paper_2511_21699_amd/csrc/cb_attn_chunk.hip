@@ -386,18 +386,234 @@ __device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& 
   return false;
 }
 
-// Tiles of up to 128 rows, four wavefronts of 32 rows, two workgroups to a compute unit: the one's start, tail and barriers are behind the
-// other's sweep.  K and V have rings of their own, a unit's K being read a step before its V, so that 72 KiB hold the unit that is
-// worked on and three that are under way.
+// Tiles of up to 256 rows in long sweeps, four wavefronts of two row tiles, one workgroup to a compute unit: an operand read from LDS serves 64
+// rows.  Units that some query does not see whole, few there, are taken one at a time and with care in any case.
+template <int D, bool PG>
+__device__ __forceinline__ void sweep_tall(const AttnParams& p, const TileJob& jb, TileLds& sh, uint4* ring) {
+  constexpr int R = 2;
+  using Part = PartialLayout<D, 32, true>;
+  using F = Feed<D, kWideWaves, 32>;
+  constexpr int NS = F::kSlots, PRO = F::kPrologue;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
+  const int r = l & 31, h = l >> 5;
+  const CB_GLOBAL uint16_t* gq = (const CB_GLOBAL uint16_t*)p.q;
+  const int S = jb.S + jb.row0 / jb.g + 1;  // (every row sees the keys below)
+  const int k0 = jb.k0, k1 = jb.k1;
+  F ring_feed(p, jb, sh.bt, ring);
+  WideFeed<D, PG> feed(ring_feed);
+  // Everything the first stages need is requested up front, oldest first: the query rows (to registers), then K/V
+  // units (to LDS).
+  TileState<D> st[R];
+  int seen[R];       // keys that the lane's queries see
+  int64_t grow[R];   // their output rows (token * Hq + head), or -1 past the end
+#pragma unroll
+  for (int t = 0; t < R; t++) {
+    int row = jb.row0 + (w * R + t) * 32 + r;
+    const bool valid = row < jb.M;
+    row = valid ? row : jb.M - 1;
+    const int token = row / jb.g;
+    seen[t] = jb.S + token + 1;
+    const int64_t gr = (int64_t)(jb.off + token) * p.Hq + jb.hk * jb.g + (row - token * jb.g);
+    grow[t] = valid ? gr : -1;
+    const CB_GLOBAL uintx4* qp = (const CB_GLOBAL uintx4*)(gq + gr * D);
+#pragma unroll
+    for (int ds = 0; ds < D / 16; ds++) st[t].q[ds] = __builtin_bit_cast(bf16x8, load_b128_untracked(qp + 2 * ds + h));
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) st[t].o[dt][v] = 0.f;
+    st[t].lacc = floatx4{0.f, 0.f, 0.f, 0.f};
+    st[t].mref = st[t].top = -INFINITY;
+    st[t].nm = 0.f;
+  }
+  const bool has_rows = jb.row0 + w * R * 32 < jb.M;
+  const float c2 = p.scale * 1.4426950408889634f;  // softmax scale in the log2 domain
+
+  const int nst = (k1 - k0 + kUnitKeys - 1) / kUnitKeys;  // stages
+  feed.request_units(nst < PRO ? nst : PRO);
+  ring_feed.wait_units(1);
+#pragma unroll
+  for (int t = 0; t < R; t++)
+#pragma unroll
+    for (int ds = 0; ds < D / 16; ds++) {
+      asm volatile("" : "+v"(st[t].q[ds]));  // (older than every unit)
+#ifdef __HIP_DEVICE_COMPILE__
+      if (R > 1) asm volatile("" : "+a"(st[t].q[ds]));  // (two tiles' queries live in accumulation registers)
+#endif
+    }
+
+  // At the barrier in front of unit u NS - 2 units from u on have been requested.  It waits until those up to u + 3 have
+  // landed; everybody is then done with those below u, whose places take the next requests.
+  // (a split of fewer units waits for all of them at the first barrier)
+  auto ready = [&] {
+    wait_vmcnt<F::kReq * (NS - 6)>();
+    bare_barrier();
+  };
+  auto first_ready = [&] {
+    const int more = (nst < NS - 2 ? nst : NS - 2) - PRO;
+    if (more > 0) feed.request_units(more);
+    if (nst < NS - 2) wait_vmcnt<0>();
+  };
+  auto top = [&] {  // of a stage in the general loop, whose last reads may still be under way
+    wait_vmcnt<F::kReq * (NS - 6)>();
+    ring_barrier();
+    feed.request_units(1);
+  };
+  // this wave's stages whose units are all prefix and all inside the split (rounds down; may be negative: none)
+  auto fast_stages = [&] {
+    const int n = ((S < k1 ? S : k1) - k0) / kUnitKeys;
+    return nst < n ? nst : n;
+  };
+  // Places in the ring, in bytes, of this wave's units of the current stage and the two behind it
+  constexpr uint32_t kSlotBytes = F::kSlotBytes;
+  auto next_place = [&](uint32_t x) { return x + kSlotBytes == NS * kSlotBytes ? 0 : x + kSlotBytes; };
+  uint32_t at = 0, at1 = next_place(at), at2 = next_place(at1);
+  auto advance = [&] {
+    at = at1;
+    at1 = at2;
+    at2 = next_place(at2);
+  };
+  const uint32_t lane_k = (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + lane_k_byte<D>(l);
+  const uint32_t lane_v = (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + kSlotBytes / 2 + lane_v_byte<D>(l);
+  const bf16x8 ones = half_ones(l);
+
+  auto unit_scores = [&](int s, uint32_t place, floatx16 (&sc)[R]) {
+    uint4 k[D / 16];
+    read_k<D>(lane_k + place, k);
+    scores<D, R>(k, st, sc);
+    const int key0 = k0 + s * kUnitKeys;
+    if (key0 + kUnitKeys > S || key0 + kUnitKeys > k1)
+#pragma unroll
+      for (int t = 0; t < R; t++) mask_chunk(sc[t], key0, seen[t], k1, h);
+  };
+  auto add_unit = [&](int s, const bf16x8 (&pb)[R][2], uint32_t place) {
+    const uint32_t va = lane_v + place;
+    const bool careful = k0 + s * kUnitKeys + kUnitKeys > S;  // (uniform)
+    bool odd = false, odd_p = false;
+    // (the denominator's MFMA has the probabilities of two queries in a column, one of them times 0)
+#pragma unroll
+    for (int t = 0; t < R; t++)
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+        st[t].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, careful ? finite_only(pb[t][j], odd_p) : pb[t][j], st[t].lacc, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; dt++) {
+        bf16x8 a = read_v<D>(va, dt, j);
+        if (careful) a = finite_only(a, odd);
+#pragma unroll
+        for (int t = 0; t < R; t++) st[t].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t][j], st[t].o[dt], 0, 0, 0);
+      }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
+#pragma unroll
+      for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + place + kSlotBytes / 2, l);
+    }
+  };
+  auto sweep = [&] {
+    floatx16 sc[R];
+    bf16x8 pb[R][2];
+    float mx[R];
+    auto check = [&] {
+      bool raise = mx[0] > st[0].top;  // (false for NaN)
+      if (R > 1) raise |= mx[R - 1] > st[R - 1].top;
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {
+#pragma unroll
+        for (int t = 0; t < R; t++) raise_reference<D>(st[t], mx[t], c2);
+      }
+    };
+    auto maxima = [&](const floatx16 (&x)[R]) {
+#pragma unroll
+      for (int t = 0; t < R; t++) mx[t] = row_max(x[t]);
+    };
+    unit_scores(0, at, sc);
+    maxima(sc);
+    check();
+    int s = 0;
+    const int fast_end = fast_stages();
+    floatx16 sd[R];
+    uint4 k[D / 16];
+    uintx4 pw[R][2];
+    bf16x8 v[D / 32];
+    // Stages whose units are all prefix, two at a time (the scores alternate between two sets of registers), the requests
+    // spread over the steps (all at once they hold up the wave that makes them).  One barrier per two units.
+    auto step = [&](const floatx16 (&from)[R], floatx16 (&to)[R], bool barrier) {  // stage s; from: its scores, to: those of stage s + 1
+      if (barrier) ready();
+      int64_t off[F::kParts];
+      uint32_t dst;
+      feed.next(off, dst);
+      score_half<D, false, R, F::kReq>(k, st, from, to, pw, lane_v + at, v, c2, [&](int i) {
+        feed.request(i, off, dst);
+      });
+      add_half<D, false, R, true>(k, lane_k + at2, lane_v + at, v, st, pw, to, mx, ones);
+      check();
+      advance();
+      s++;
+    };
+    first_ready();
+    if (s + 2 < fast_end) {
+      ready();  // (K operands are a step ahead in registers)
+      read_k<D>(lane_k + at1, k);
+      do {
+        step(sc, sd, true);
+        step(sd, sc, false);
+      } while (s + 2 < fast_end);
+    }
+    for (; s + 1 < nst; s++) {
+      top();
+      floatx16 sn[R];
+      unit_scores(s + 1, at1, sn);
+#pragma unroll
+      for (int t = 0; t < R; t++) probs<D, false>(sc[t], st[t], c2, pb[t]);
+      add_unit(s, pb, at);
+      maxima(sn);
+      check();
+#pragma unroll
+      for (int t = 0; t < R; t++) sc[t] = sn[t];
+      advance();
+    }
+#pragma unroll
+    for (int t = 0; t < R; t++) probs<D, false>(sc[t], st[t], c2, pb[t]);
+    add_unit(s, pb, at);
+  };
+  if (has_rows) sweep();
+  else {  // no rows of its own: it only brings its share, passing the same barriers
+    int s = 0;
+    first_ready();
+    const int fast_end = fast_stages();
+    if (s + 2 < fast_end) ready();
+    for (; s + 2 < fast_end; s += 2) {
+      ready();
+      feed.request_units(2);
+    }
+    for (; s + 1 < nst; s++) top();
+  }
+  wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
+#pragma unroll
+  for (int t = 0; t < R; t++) {
+    floatx4 f[Part::P];
+#pragma unroll
+    for (int pc = 0; pc < Part::P; pc++) {
+      const floatx16& o = st[t].o[pc >> 2];
+      f[pc] = floatx4{o[4 * (pc & 3)], o[4 * (pc & 3) + 1], o[4 * (pc & 3) + 2], o[4 * (pc & 3) + 3]};
+    }
+    write_rows<D, 32, true, Part::P>(p, jb, w * R + t, grow[t], f, 0, st[t].mref, st[t].lacc[0], c2, true, l);
+  }
+}
+
+// Tiles of up to 128 rows, four wavefronts of 32 rows, two workgroups to a compute unit: the one's start, tail and barriers are behind
+// the other's sweep.  K and V have rings of their own, a unit's K being read a step before its V, so that 72 KiB hold what is worked on
+// and two units that are under way.
 template <int D>
 struct ManyLds {
-  static constexpr int kK = 4, kV = 5;                          // units
+  static constexpr int kK = 5, kV = 4;                          // units
   static constexpr int kBytes = kUnitKeys * D * 2;              // of a unit's K, or V
   uint4 ring[(kK + kV) * kBytes / 16];
   int bt[kBtLds];
   int flag;
 };
 
+// The memory side: K of a unit is requested two steps before its V, whose addresses wait in registers until then.
 template <int D, bool PG>
 struct ManyFeed {
   using F = Feed<D, kWideWaves, 32>;
@@ -410,6 +626,7 @@ struct ManyFeed {
   const CB_GLOBAL char *kb[P], *vb[P];   // what the row's offset is added to
   uint32_t k_place = 0, v_place = 0;     // of the next unit in the rings, bytes
   int blk[P];                            // paged: the rows' entries of the block table
+  int64_t off[P], later[2][P];           // offsets of the unit whose K is next, and of the two whose V are
   __device__ __forceinline__ explicit ManyFeed(F& feed) : f(feed), last(feed.jb.k1 - 1) {
     const AttnParams& p = f.p;
     const int lr = f.l / F::VPR, lc = f.l % F::VPR;
@@ -422,6 +639,7 @@ struct ManyFeed {
       kb[i] = f.kbase + head + (lc ^ swizzle_k<D>(rr)) * 16;
       vb[i] = f.vbase + head + (lc ^ swizzle_v<D, 32>(rr)) * 16;
       blk[i] = 0;
+      later[0][i] = later[1][i] = 0;
     }
     if (PG) look_up();
   }
@@ -429,8 +647,8 @@ struct ManyFeed {
 #pragma unroll
     for (int i = 0; i < P; i++) blk[i] = f.bt[((key[i] >> f.ka.bs_shift) - f.ka.bt_first) & (kBtLds - 1)];
   }
-  // The next unit's addresses, and on to the one behind it (whose table entries are asked for here and looked at a step later).
-  __device__ __forceinline__ void next(int64_t (&off)[P], uint32_t& kd, uint32_t& vd) {
+  // The next unit's offsets, and on to the one behind it (whose table entries are asked for here and looked at a step later).
+  __device__ __forceinline__ void next() {
     const KvAddr& a = f.p.kv;
     if (PG) {
       if (f.long_slice) f.bt_ahead(f.requested);
@@ -450,24 +668,29 @@ struct ManyFeed {
       key[i] = key[i] < last ? key[i] : last;
     }
     if (PG) look_up();
-    const uint32_t at = f.part_row(0) * (2 * D) + __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(CB_LDS uint4*)f.ring);
-    kd = at + k_place;
-    vd = at + v_place + L::kK * L::kBytes;
-    k_place = k_place + L::kBytes == L::kK * L::kBytes ? 0 : k_place + L::kBytes;
-    v_place = v_place + L::kBytes == L::kV * L::kBytes ? 0 : v_place + L::kBytes;
     f.requested++;
   }
-  // request i of a unit's 2 P (a constant): the groups' K, then their V
-  __device__ __forceinline__ void request(int i, const int64_t (&off)[P], uint32_t kd, uint32_t vd) const {
-    const int part = i % P;
-    lds_dma_b128_at((i < P ? kb[part] : vb[part]) + off[part], (i < P ? kd : vd) + part * (RPR * 2 * D));
+  __device__ __forceinline__ uint32_t lds_at() const { return f.part_row(0) * (2 * D) + __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(CB_LDS uint4*)f.ring); }
+  // request i of a step's 2 P (a constant): K's groups, then those of the V that is due
+  __device__ __forceinline__ void request(int i) const {
+    if (i < P) lds_dma_b128_at(kb[i] + off[i], lds_at() + k_place + i * (RPR * 2 * D));
+    else lds_dma_b128_at(vb[i - P] + later[0][i - P], lds_at() + v_place + L::kK * L::kBytes + (i - P) * (RPR * 2 * D));
   }
-  __device__ __forceinline__ void request_unit() {
-    int64_t off[P];
-    uint32_t kd, vd;
-    next(off, kd, vd);
+  __device__ __forceinline__ void requested(bool k, bool v) {  // which of the two a step has made
+    if (k) k_place = k_place + L::kBytes == L::kK * L::kBytes ? 0 : k_place + L::kBytes;
+    if (v) v_place = v_place + L::kBytes == L::kV * L::kBytes ? 0 : v_place + L::kBytes;
 #pragma unroll
-    for (int i = 0; i < 2 * P; i++) request(i, off, kd, vd);
+    for (int i = 0; i < P; i++) {
+      later[0][i] = later[1][i];
+      later[1][i] = off[i];
+    }
+  }
+  __device__ __forceinline__ void request_step(bool v = true) {
+    next();
+#pragma unroll
+    for (int i = 0; i < 2 * P; i++)
+      if (v || i < P) request(i);
+    requested(true, v);
   }
 };
 
@@ -477,44 +700,53 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
   using Part = PartialLayout<D, 32, true>;
   using F = Feed<D, kWideWaves, 32>;
   using L = ManyLds<D>;
+  constexpr int R = 1;  // row tiles of a wavefront
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, r = l & 31, h = l >> 5;
   const CB_GLOBAL uint16_t* gq = (const CB_GLOBAL uint16_t*)p.q;
   const int S = jb.S + jb.row0 / jb.g + 1;  // (every row sees the keys below)
   const int k0 = jb.k0, k1 = jb.k1;
   F ring_feed(p, jb, sh.bt, sh.ring);
   ManyFeed<D, PG> feed(ring_feed);
-  TileState<D> st[1];
-  int row = jb.row0 + w * 32 + r;
-  const bool valid = row < jb.M;
-  row = valid ? row : jb.M - 1;
-  const int token = row / jb.g, seen = jb.S + token + 1;
-  const int64_t gr = (int64_t)(jb.off + token) * p.Hq + jb.hk * jb.g + (row - token * jb.g), grow = valid ? gr : -1;
-  const CB_GLOBAL uintx4* qp = (const CB_GLOBAL uintx4*)(gq + gr * D);
+  TileState<D> st[R];
+  int seen[R];       // keys that the lane's queries see
+  int64_t grow[R];   // their output rows (token * Hq + head), or -1 past the end
 #pragma unroll
-  for (int ds = 0; ds < D / 16; ds++) st[0].q[ds] = __builtin_bit_cast(bf16x8, load_b128_untracked(qp + 2 * ds + h));
+  for (int t = 0; t < R; t++) {
+    int row = jb.row0 + (w * R + t) * 32 + r;
+    const bool valid = row < jb.M;
+    row = valid ? row : jb.M - 1;
+    const int token = row / jb.g;
+    seen[t] = jb.S + token + 1;
+    const int64_t gr = (int64_t)(jb.off + token) * p.Hq + jb.hk * jb.g + (row - token * jb.g);
+    grow[t] = valid ? gr : -1;
+    const CB_GLOBAL uintx4* qp = (const CB_GLOBAL uintx4*)(gq + gr * D);
 #pragma unroll
-  for (int dt = 0; dt < D / 32; dt++)
+    for (int ds = 0; ds < D / 16; ds++) st[t].q[ds] = __builtin_bit_cast(bf16x8, load_b128_untracked(qp + 2 * ds + h));
 #pragma unroll
-    for (int v = 0; v < 16; v++) st[0].o[dt][v] = 0.f;
-  st[0].lacc = floatx4{0.f, 0.f, 0.f, 0.f};
-  st[0].mref = st[0].top = -INFINITY;
-  st[0].nm = 0.f;
-  const bool has_rows = jb.row0 + w * 32 < jb.M;
+    for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) st[t].o[dt][v] = 0.f;
+    st[t].lacc = floatx4{0.f, 0.f, 0.f, 0.f};
+    st[t].mref = st[t].top = -INFINITY;
+    st[t].nm = 0.f;
+  }
+  const bool has_rows = jb.row0 + w * R * 32 < jb.M;
   const float c2 = p.scale * 1.4426950408889634f;  // softmax scale in the log2 domain
   const int nst = (k1 - k0 + kUnitKeys - 1) / kUnitKeys;
-  for (int u = 0; u < L::kK; u++) feed.request_unit();  // (past the split's end: its last key)
-  wait_vmcnt<F::kReq * L::kK - F::kReq / 2>();
+  // K of five units and V of three (past the split's end: its last key); the first two units' K have landed at the first barrier
+  feed.request_step(false);
+  feed.request_step(false);
+  for (int u = 0; u < 3; u++) feed.request_step();
+  wait_vmcnt<3 * F::kReq>();
   ring_barrier();
 #pragma unroll
-  for (int ds = 0; ds < D / 16; ds++) asm volatile("" : "+v"(st[0].q[ds]));  // (older than every unit)
-  // At the barrier of step s units up to s + 3 have been requested, and K up to s + 1 and V up to s have landed; everybody is done with K(s) and
-  // V(s - 1), whose places take those of unit s + 4.
+  for (int t = 0; t < R; t++)
+#pragma unroll
+    for (int ds = 0; ds < D / 16; ds++) asm volatile("" : "+v"(st[t].q[ds]));  // (older than every unit)
+  // At the barrier of step s K up to unit s + 4 and V up to s + 2 have been requested, and K up to s + 2 and V up to s have landed; everybody is
+  // done with K(s) and V(s - 1) (reads of K(s + 1) may be under way), whose places take K(s + 5) and V(s + 3).
   auto ready = [&] {
-    wait_vmcnt<F::kReq / 2 + 2 * F::kReq>();
-    bare_barrier();
-  };
-  auto last_ready = [&] {  // (the last unit's V)
-    wait_vmcnt<3 * F::kReq>();
+    wait_vmcnt<2 * F::kReq>();
     bare_barrier();
   };
   const int whole_end = S < k1 ? S : k1;
@@ -523,7 +755,7 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
   const uint32_t ring = (uint32_t)(uintptr_t)(CB_LDS uint4*)sh.ring, vring = ring + L::kK * L::kBytes;
   const uint32_t lane_k = ring + lane_k_byte<D>(l), lane_v = vring + lane_v_byte<D>(l);
   const bf16x8 ones = half_ones(l);
-  uint32_t k_at = 0, v_at = 0;  // places of K(s + 1) and V(s); K's is that of K(0) at first
+  uint32_t k_at = 0, v_at = 0;  // places of the K that is read next and of V(s)
   auto advance_k = [&] { k_at = k_at + L::kBytes == L::kK * L::kBytes ? 0 : k_at + L::kBytes; };
   auto advance_v = [&] { v_at = v_at + L::kBytes == L::kV * L::kBytes ? 0 : v_at + L::kBytes; };
   uint32_t odd = 0;  // bits 15 and 31: infinities or NaN
@@ -534,41 +766,51 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
     for (uint32_t x = 0; x < kShare; x += 1024) odd = odd_bits(__builtin_bit_cast(uintx4, *(const CB_LDS uintx4*)(vring + v_at + w * kShare + x + l * 16)), odd);
     asm volatile("" : "+v"(odd));  // (the reads are through before the next barrier)
   };
-  auto mask = [&](int s, floatx16 (&sc)[1]) {
-    if (masked(s)) mask_chunk(sc[0], k0 + s * kUnitKeys, seen, k1, h);
+  auto mask = [&](int s, floatx16 (&sc)[R]) {
+    if (!masked(s)) return;
+#pragma unroll
+    for (int t = 0; t < R; t++) mask_chunk(sc[t], k0 + s * kUnitKeys, seen[t], k1, h);
   };
-  auto raise = [&](float mx) {  // (false for NaN)
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > st[0].top) != 0, 0)) raise_reference<D>(st[0], mx, c2);
+  auto check = [&](const float (&mx)[R]) {
+    bool raise = mx[0] > st[0].top;  // (false for NaN)
+    if (R > 1) raise |= mx[R - 1] > st[R - 1].top;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {
+#pragma unroll
+      for (int t = 0; t < R; t++) raise_reference<D>(st[t], mx[t], c2);
+    }
   };
   auto sweep = [&] {
-    floatx16 sc[1], sd[1];
-    float mx[1];
+    floatx16 sc[R], sd[R];
+    float mx[R];
     uint4 k[D / 16];
-    uintx4 pw[1][2];
+    uintx4 pw[R][2];
     bf16x8 v[D / 32];
     auto odd_max = [&](int s) {
-      if (hides && masked(s)) odd |= mx[0] < INFINITY ? 0u : 0x8000u;
+      if (!hides || !masked(s)) return;
+#pragma unroll
+      for (int t = 0; t < R; t++) odd |= mx[t] < INFINITY ? 0u : 0x8000u;
     };
     read_k<D>(lane_k, k);
-    scores<D, 1>(k, st, sc);
+    scores<D, R>(k, st, sc);
     mask(0, sc);
-    mx[0] = row_max(sc[0]);
+#pragma unroll
+    for (int t = 0; t < R; t++) mx[t] = row_max(sc[t]);
     odd_max(0);
-    raise(mx[0]);
+    check(mx);
     advance_k();
-    // A step: the scores of unit s + 1 beside the exponentials of unit s, then its values.
-    auto step = [&](int s, const floatx16 (&from)[1], floatx16 (&to)[1], bool masks) {  // from: the scores of unit s, to: those of unit s + 1
+    read_k<D>(lane_k + k_at, k);
+    advance_k();
+    // A step: the scores of unit s + 1 beside the exponentials of unit s, then its values, beside which K of unit s + 2 is read.
+    auto step = [&](int s, const floatx16 (&from)[R], floatx16 (&to)[R], bool masks) {  // from: the scores of unit s, to: those of unit s + 1
       ready();
-      read_k<D>(lane_k + k_at, k);
       if (masks) look(s);
-      int64_t off[F::kParts];
-      uint32_t kd, vd;
-      feed.next(off, kd, vd);
-      score_half<D, false, 1, F::kReq>(k, st, from, to, pw, lane_v + v_at, v, c2, [&](int i) { feed.request(i, off, kd, vd); });
+      feed.next();
+      score_half<D, false, R, F::kReq>(k, st, from, to, pw, lane_v + v_at, v, c2, [&](int i) { feed.request(i); });
+      feed.requested(true, true);
       if (masks) mask(s + 1, to);
-      add_half<D, false, 1, false>(k, 0, lane_v + v_at, v, st, pw, to, mx, ones);
+      add_half<D, false, R, true>(k, lane_k + k_at, lane_v + v_at, v, st, pw, to, mx, ones);
       if (masks) odd_max(s + 1);
-      raise(mx[0]);
+      check(mx);
       advance_k();
       advance_v();
     };
@@ -579,45 +821,61 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
     }
     for (; s + 1 < nst; s++) {
       step(s, sc, sd, true);
-      sc[0] = sd[0];
-    }
-    last_ready();
-    look(s);
-    bf16x8 pb[2];
-    probs<D, false>(sc[0], st[0], c2, pb);
 #pragma unroll
-    for (int j = 0; j < 2; j++) st[0].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[j], st[0].lacc, 0, 0, 0);
+      for (int t = 0; t < R; t++) sc[t] = sd[t];
+    }
+    ready();
+    look(s);
+    bf16x8 pb[R][2];
+#pragma unroll
+    for (int t = 0; t < R; t++) {
+      probs<D, false>(sc[t], st[t], c2, pb[t]);
+#pragma unroll
+      for (int j = 0; j < 2; j++) st[t].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[t][j], st[t].lacc, 0, 0, 0);
+    }
 #pragma unroll
     for (int j = 0; j < 2; j++)
 #pragma unroll
-      for (int dt = 0; dt < D / 32; dt++) st[0].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v<D>(lane_v + v_at, dt, j), pb[j], st[0].o[dt], 0, 0, 0);
+      for (int dt = 0; dt < D / 32; dt++) {
+        const bf16x8 a = read_v<D>(lane_v + v_at, dt, j);
+#pragma unroll
+        for (int t = 0; t < R; t++) st[t].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t][j], st[t].o[dt], 0, 0, 0);
+      }
   };
   auto careful_sweep = [&] {  // a unit at a time
-    if (has_rows)
-#pragma unroll
-      for (int dt = 0; dt < D / 32; dt++) asm volatile("" : "+v"(st[0].o[dt]));
     for (int s = 0; s < nst; s++) {
       wait_vmcnt<0>();
       ring_barrier();
-      if (s > 0) feed.request_unit();
+      if (s > 0) feed.request_step();
       if (has_rows) {
         uint4 k[D / 16];
-        floatx16 sc[1];
-        bf16x8 pb[2];
+        floatx16 sc[R];
+        bf16x8 pb[R][2];
+        float mx[R];
         bool odd_v = false, odd_p = false;
         read_k<D>(lane_k + k_at, k);
-        scores<D, 1>(k, st, sc);
+        scores<D, R>(k, st, sc);
         mask(s, sc);
-        raise(row_max(sc[0]));
-        probs<D, false>(sc[0], st[0], c2, pb);
 #pragma unroll
-        for (int j = 0; j < 2; j++) st[0].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, finite_only(pb[j], odd_p), st[0].lacc, 0, 0, 0);
+        for (int t = 0; t < R; t++) mx[t] = row_max(sc[t]);
+        check(mx);
+#pragma unroll
+        for (int t = 0; t < R; t++) {
+          probs<D, false>(sc[t], st[t], c2, pb[t]);
+#pragma unroll
+          for (int j = 0; j < 2; j++) st[t].lacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, finite_only(pb[t][j], odd_p), st[t].lacc, 0, 0, 0);
+        }
 #pragma unroll
         for (int j = 0; j < 2; j++)
 #pragma unroll
-          for (int dt = 0; dt < D / 32; dt++)
-            st[0].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_only(read_v<D>(lane_v + v_at, dt, j), odd_v), pb[j], st[0].o[dt], 0, 0, 0);
-        if (__builtin_amdgcn_ballot_w64(odd_v) != 0) add_odd_values<D>(st[0].o, pb[0], pb[1], vring + v_at, l);
+          for (int dt = 0; dt < D / 32; dt++) {
+            const bf16x8 a = finite_only(read_v<D>(lane_v + v_at, dt, j), odd_v);
+#pragma unroll
+            for (int t = 0; t < R; t++) st[t].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t][j], st[t].o[dt], 0, 0, 0);
+          }
+        if (__builtin_amdgcn_ballot_w64(odd_v) != 0)
+#pragma unroll
+          for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], vring + v_at, l);
       }
       advance_k();
       advance_v();
@@ -629,10 +887,10 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
     for (int s = 0; s + 1 < nst; s++) {
       ready();
       look(s);
-      feed.request_unit();
+      feed.request_step();
       advance_v();
     }
-    last_ready();
+    ready();
     look(nst - 1);
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
@@ -643,13 +901,16 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
     __syncthreads();
     if (sh.flag) return true;
   }
-  floatx4 f[Part::P];
 #pragma unroll
-  for (int pc = 0; pc < Part::P; pc++) {
-    const floatx16& o = st[0].o[pc >> 2];
-    f[pc] = floatx4{o[4 * (pc & 3)], o[4 * (pc & 3) + 1], o[4 * (pc & 3) + 2], o[4 * (pc & 3) + 3]};
+  for (int t = 0; t < R; t++) {
+    floatx4 f[Part::P];
+#pragma unroll
+    for (int pc = 0; pc < Part::P; pc++) {
+      const floatx16& o = st[t].o[pc >> 2];
+      f[pc] = floatx4{o[4 * (pc & 3)], o[4 * (pc & 3) + 1], o[4 * (pc & 3) + 2], o[4 * (pc & 3) + 3]};
+    }
+    write_rows<D, 32, true, Part::P>(p, jb, w * R + t, grow[t], f, 0, st[t].mref, st[t].lacc[0], c2, true, l);
   }
-  write_rows<D, 32, true, Part::P>(p, jb, w, grow, f, 0, st[0].mref, st[0].lacc[0], c2, true, l);
   return false;
 }
 
@@ -664,6 +925,19 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_few(AttnParams p_a
   if (!chunk_job(p, ml, blockIdx.x, jb)) return;
   if (sweep_chunk<D, PG, 1, 2, false>(p, jb, sh, ring)) sweep_chunk<D, PG, 1, 2, true>(p, jb, sh, ring);
   if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
+}
+
+template <int D, bool PG>
+__global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_tall(AttnParams p_arg, SeqMeta meta) {
+  const SeqMetaLanes ml = seq_meta_prefetch(meta);
+  __shared__ __align__(1024) uint4 ring[Feed<D, kWideWaves, 32>::kRingVecs];
+  __shared__ TileLds sh;
+  AttnParams p = p_arg;
+  pin_args(p);
+  TileJob jb;
+  if (!chunk_job(p, ml, blockIdx.x, jb)) return;
+  sweep_tall<D, PG>(p, jb, sh, ring);
+  if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 256, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
 }
 
 template <int D, bool PG>
@@ -692,8 +966,10 @@ static hipError_t launch_dim(hipStream_t st, const AttnParams& p, const SeqMeta&
   const bool paged = p.kv.block_size > 0;
   if (p.tile_rows == 64 && paged) hipLaunchKernelGGL((k_chunk_few<D, true>), grid, block, 0, st, p, meta);
   else if (p.tile_rows == 64) hipLaunchKernelGGL((k_chunk_few<D, false>), grid, block, 0, st, p, meta);
-  else if (paged) hipLaunchKernelGGL((k_chunk_many<D, true>), grid, block, 0, st, p, meta);
-  else hipLaunchKernelGGL((k_chunk_many<D, false>), grid, block, 0, st, p, meta);
+  else if (p.tile_rows == 128 && paged) hipLaunchKernelGGL((k_chunk_many<D, true>), grid, block, 0, st, p, meta);
+  else if (p.tile_rows == 128) hipLaunchKernelGGL((k_chunk_many<D, false>), grid, block, 0, st, p, meta);
+  else if (paged) hipLaunchKernelGGL((k_chunk_tall<D, true>), grid, block, 0, st, p, meta);
+  else hipLaunchKernelGGL((k_chunk_tall<D, false>), grid, block, 0, st, p, meta);
   return hipGetLastError();
 }
 hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs) {

@@ -4,10 +4,16 @@
 
 namespace cb {
 
-// The workgroup's (tile, split).  Workgroups are numbered sequence by sequence, the longest first, a sequence's tiles from the last, whose
+// The workgroup's (tile, split).  p.grid_x: workgroups.  They are numbered sequence by sequence, the longest first, a sequence's tiles from the last, whose
 // sweep is the longest, to the first, then splits, and the kv head runs fastest: what is dispatched last is short, and with a
 // multiple of 8 kv heads a head's tiles share an XCD's L2.
 __device__ __forceinline__ bool chunk_job(const AttnParams& p, const SeqMetaLanes& ml, int d, TileJob& j) {
+  // Two workgroups to a compute unit: numbers 256 to 511 go where 0 to 255 have gone, in that order, so they are taken from the shortest on, in
+  // stretches of 8 that keep their XCD (a prompt of 2048, 32 heads: 64 stages and 1 on a compute unit instead of 64 and 32).
+  if (d >= 256 && d < 512 && p.grid_x % 8 == 0) {
+    const int end = p.grid_x < 512 ? p.grid_x : 512;
+    d = 256 + end - 8 - (d & ~7) + (d & 7);
+  }
   const int i = __popcll(__builtin_amdgcn_ballot_w64(ml.start <= d)) - 1;  // (starts past the batch are INT_MAX)
   j.b = __builtin_amdgcn_readlane(ml.ord, i);
   const int at = d - __builtin_amdgcn_readlane(ml.start, i);

@@ -339,6 +339,9 @@ extern "C" int cb_debug_layers(const cb_config* cfg, int32_t layers, int32_t bat
 extern "C" int cb_debug_step(cb_ctx* ctx, int32_t info[4]);
 // The pool size that the kernels clamp the block table's entries to (0: contiguous, -1: unknown layout).
 extern "C" int64_t cb_debug_pool_blocks(const cb_config* cfg, const cb_kv_layer* layer);
+// How a chunk's attention is cut up (splits, tile_rows: the options, 0 = automatic): plan[0] = rows of a tile, [1] = splits of the longest, [2] = keys per split,
+// [3] = workgroups, [4] = row tiles of the longest chunk per kv head
+extern "C" int cb_debug_chunk_plan(const cb_config* cfg, int32_t batch, const int32_t* kv_len, const int32_t* token_offsets, int32_t splits, int32_t tile_rows, int32_t plan[5]);
 // The argument checks of the calls around the verification (err: 256 bytes).
 extern "C" int cb_debug_check_append(const cb_config* cfg, int32_t batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                      int64_t v_stride, const cb_head_prep* prep, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets,
