@@ -1082,17 +1082,19 @@ bool layers_together(cb_ctx* ctx, int batch, int n, const void* const* q, const 
   return true;
 }
 
-// How a chunk's attention is cut up: tiles of so many rows, each over its keys in splits of `chunk`.
+// How a chunk's attention is cut up: tiles of so many rows, each over its keys in splits.
 struct ChunkPlan {
-  int tile_rows, chunk, nsplit;  // nsplit: of the longest tile
-  int64_t jobs;                  // workgroups
-  int tiles;                     // row tiles of the longest chunk, per kv head
+  int tile_rows, nsplit;  // nsplit: of the longest tile
+  int64_t jobs;           // workgroups
+  int tiles;              // row tiles of the longest chunk, per kv head
+  ChunkSplits splits;
 };
 
-// The cheapest of a few plans by an estimate of the launch's time.  A workgroup takes `start` us beside its sweep and `unit` us for every
-// 32 keys; the longest are dispatched first, so the launch ends no later than max(longest job, work / 256 compute units + the shortest job),
-// nor before the cache has been read.  Splits are for launches that leave compute units idle; their partial states have the room that
-// the workspace has.
+// The cheapest of a few plans by an estimate of the launch's time, in us.  A sequence is cut into as many equal splits as its length has of the
+// longest's, so that jobs are of about one length.  A job takes `start` beside its sweep and `alone` for every 32 keys where it has a compute
+// unit for itself; a compute unit gets through 32 keys of a tile in `full`, with as many workgroups as it holds, at the clock of a busy chip.  The longest
+// are dispatched first, so the launch ends with the longest job or, where there are more than compute units, when the work is shared out and a job of
+// the shortest is through; nor before the cache has been read.  Splits have the room that the workspace has.
 ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, int opt_tile_rows, int batch, const int32_t* kv_len, const int32_t* off) {
   const bool f32 = c.qkv_dtype == CB_F32;
   const int g = c.num_q_heads / c.num_kv_heads, Hkv = c.num_kv_heads;
@@ -1105,7 +1107,7 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     len_max = std::max(len_max, kv_len[b] + n);
     slots += kv_len[b] + n;
   }
-  const double memory = slots * Hkv * c.head_dim * (f32 ? 8 : 4) / 5.3e6 + 3.0, by_dim = c.head_dim == 128 ? 1.0 : 0.6;
+  const double memory = slots * Hkv * c.head_dim * (f32 ? 8 : 4) / 4.6e6 + 3.0, by_dim = c.head_dim == 128 ? 1.0 : 0.6;
   const int64_t m_max = (int64_t)n_max * g, total = off[batch];
   // A split's partial states, and tiles that there are tickets for.  (Within a sequence the bf16 kernel's offsets have 31 bits.)
   const int64_t per_split = f32 ? total * c.num_q_heads * partial_stride(c.head_dim) * 4 : chunk_partial_bytes(c.head_dim, total, c.num_q_heads, Hkv, batch);
@@ -1113,17 +1115,18 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
   const int64_t most_here = f32 ? INT32_MAX : ((1ll << 31) - 1) / chunk_partial_bytes(c.head_dim, n_max, c.num_q_heads, Hkv, 2);
   struct Tile {
     int rows;
-    double unit, start;
+    double alone, full, start, merge;
   };
-  static const Tile kBf16[] = {{64, 0.38, 5.0}, {128, 0.5, 4.0}, {256, 0.95, 6.0}}, kF32[] = {{16, 0.43, 3.0}, {32, 0.8, 4.0}};
+  // (4096 to 8192 tokens, and 256 behind 30000, 32/8 heads; the fp32 ones 512 behind 4096)
+  static const Tile kBf16[] = {{64, 0.36, 0.36, 4.0, 2.0}, {128, 0.66, 0.52, 5.0, 3.0}, {256, 0.86, 0.96, 7.0, 5.0}};
+  static const Tile kF32[] = {{16, 0.43, 0.43, 3.0, 2.5}, {32, 0.8, 0.8, 4.0, 3.0}};
   ChunkPlan best{};
   double best_us = 0;
   for (int kind = 0; kind < (f32 ? 2 : 3); kind++) {
     const Tile& tile = f32 ? kF32[kind] : kBf16[kind];
     const int rows = tile.rows;
-    if (best.jobs && m_max <= rows / 2) break;
-    if (!f32 && opt_tile_rows && rows != opt_tile_rows && m_max > 64) continue;
-    const double unit = tile.unit * by_dim, start = tile.start;
+    if (opt_tile_rows && !f32 ? rows != opt_tile_rows : best.jobs && m_max <= rows / 2) continue;
+    const double alone = tile.alone * by_dim, full = tile.full * by_dim, start = tile.start;
     const int tiles_max = (int)((m_max + rows - 1) / rows);
     int64_t tiles = 0;
     for (int b = 0; b < batch; b++) tiles += ((int64_t)(off[b + 1] - off[b]) * g + rows - 1) / rows * Hkv;
@@ -1135,15 +1138,19 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
       ns = std::min(ns, most);
       if (ns == last) break;
       last = ns;
-      const int chunk = ((len_max + ns - 1) / ns + 31) / 32 * 32;
-      double work = 0, longest = 0, shortest = 1e30;
-      int64_t jobs = 0, real = 0, merged = 0;
+      const int target = (len_max + ns - 1) / ns;
+      ChunkPlan p{rows, 1, 0, tiles_max, {}};
+      double work = 0, longest = 0, shortest = 1e30;  // in units of 32 keys
+      int64_t real = 0, merged = 0;
       for (int b = 0; b < batch; b++) {
-        const int n = off[b + 1] - off[b], s = kv_len[b], nt = (int)(((int64_t)n * g + rows - 1) / rows);
+        const int n = off[b + 1] - off[b], s = kv_len[b], len = s + n, nt = (int)(((int64_t)n * g + rows - 1) / rows);
         if (n == 0) continue;
-        jobs += (int64_t)nt * Hkv * ((s + n + chunk - 1) / chunk);
-        if (ns == 1) {  // (whole tiles: their lengths are evenly spaced)
-          const double first = start + unit * ((s + std::min(n, (rows + g - 1) / g) + 31) / 32), end = start + unit * ((s + n + 31) / 32);
+        const int parts = (len + target - 1) / target, chunk = ((len + parts - 1) / parts + 31) / 32 * 32, ns_b = (len + chunk - 1) / chunk;
+        p.splits.keys[b] = chunk;
+        p.nsplit = std::max(p.nsplit, ns_b);
+        p.jobs += (int64_t)nt * Hkv * ns_b;
+        if (ns_b == 1) {  // (whole tiles: their lengths are evenly spaced)
+          const double first = (s + std::min(n, (rows + g - 1) / g) + 31) / 32, end = (len + 31) / 32;
           work += 0.5 * (first + end) * nt * Hkv;
           longest = std::max(longest, end);
           shortest = std::min(shortest, first);
@@ -1151,19 +1158,21 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
           continue;
         }
         for (int t = 0; t < nt; t++) {
-          const int len = s + (int)((std::min<int64_t>((int64_t)(t + 1) * rows, (int64_t)n * g) - 1) / g) + 1, full = len / chunk, rest = len - full * chunk;
-          const double f = start + unit * (chunk / 32), r = rest ? start + unit * ((rest + 31) / 32) : 1e30;
-          work += (full * f + (rest ? r : 0.0)) * Hkv;
-          longest = std::max(longest, full ? f : r);
-          shortest = std::min(shortest, std::min(full ? f : 1e30, r));
-          real += (int64_t)(full + (rest > 0)) * Hkv;
-          merged += (full + (rest > 0)) > 1 ? Hkv : 0;
+          const int tl = s + (int)((std::min<int64_t>((int64_t)(t + 1) * rows, (int64_t)n * g) - 1) / g) + 1, whole = tl / chunk, rest = tl - whole * chunk;
+          work += (whole * (chunk / 32) + (rest + 31) / 32) * (double)Hkv;
+          longest = std::max(longest, (double)(whole ? chunk / 32 : (rest + 31) / 32));
+          shortest = std::min(shortest, (double)(rest ? (rest + 31) / 32 : chunk / 32));
+          real += (int64_t)(whole + (rest > 0)) * Hkv;
+          merged += whole + (rest > 0) > 1 ? Hkv : 0;
         }
       }
-      const double merge = ns == 1 ? 0.0 : real <= 256 ? 1.5 : 2.0 + 0.4 * ns * (rows / 128.0);
-      const double us = std::max(memory + (ns > 1 ? merge : 0.0), real <= 256 ? longest + merge : std::max(longest + merge, (work + merged * merge) / 256 + shortest));
-      if (best.jobs == 0 || us < best_us - 0.2) {
-        best = ChunkPlan{rows, chunk, (len_max + chunk - 1) / chunk, jobs, tiles_max};
+      const double merge = p.nsplit == 1 ? 0.0 : real <= 256 ? 1.5 : tile.merge + 0.15 * p.nsplit;
+      const double one = longest * alone + start + merge;
+      const bool two = rows == 128 && !f32;  // (workgroups to a compute unit, whose starts and tails hide behind each other)
+      const double shared = (work * full + real * (two ? 0.3 : 1.0) * start + merged * merge * (two ? 0.5 : 1.0)) / 256 + shortest * full + (two ? start : 0.0);
+      const double us = std::max(memory + merge, real <= 256 ? one : std::max(one, shared));
+      if (best.jobs == 0 || us < best_us * 0.99 - 0.1) {
+        best = p;
         best_us = us;
       }
       if (opt_splits > 0) break;
@@ -1806,7 +1815,7 @@ int cb_chunk_attention_device(cb_ctx* ctx, void* hip_stream, int32_t batch, cons
     if (i >= batch) continue;
     const int b = meta.by_length[i];
     const int64_t rows = (int64_t)(token_offsets[b + 1] - token_offsets[b]) * (c.num_q_heads / c.num_kv_heads);
-    before += (rows + plan.tile_rows - 1) / plan.tile_rows * c.num_kv_heads * ((len(b) + plan.chunk - 1) / plan.chunk);
+    if (rows > 0) before += (rows + plan.tile_rows - 1) / plan.tile_rows * c.num_kv_heads * ((len(b) + plan.splits.keys[b] - 1) / plan.splits.keys[b]);
   }
   AttnParams p{};
   p.q = q;
@@ -1816,7 +1825,7 @@ int cb_chunk_attention_device(cb_ctx* ctx, void* hip_stream, int32_t batch, cons
   p.tickets = ctx->dev<uint32_t>(ctx->lay.tickets);
   p.coop_tickets = ctx->dev<uint32_t>(ctx->lay.coop_tickets);
   p.Hq = c.num_q_heads, p.Hkv = c.num_kv_heads, p.D = c.head_dim;
-  p.chunk = plan.chunk, p.nsplit = plan.nsplit, p.tile_rows = plan.tile_rows;
+  p.nsplit = plan.nsplit, p.tile_rows = plan.tile_rows;
   p.batch = batch;
   p.scale = a.scale;
   p.grid_x = (int32_t)plan.jobs;
@@ -1825,7 +1834,7 @@ int cb_chunk_attention_device(cb_ctx* ctx, void* hip_stream, int32_t batch, cons
   p.status = ctx->dev<int32_t>(ctx->lay.status);
   // (the whole launch resident at once, a workgroup to a compute unit: see split_merge)
   p.coop_merge = ctx->opt_coop && plan.nsplit > 1 && plan.nsplit <= 64 && plan.jobs <= 256 && (int64_t)batch * c.num_kv_heads * plan.tiles <= kCoopTiles;
-  CB_LAUNCH(ctx, f32 ? launch_attn_chunk_f32(st, p, meta, (int)plan.jobs) : launch_attn_chunk(st, p, meta, (int)plan.jobs));
+  CB_LAUNCH(ctx, f32 ? launch_attn_chunk_f32(st, p, meta, plan.splits, (int)plan.jobs) : launch_attn_chunk(st, p, meta, plan.splits, (int)plan.jobs));
   return CB_OK;
 }
 
@@ -1864,7 +1873,7 @@ int cb_debug_chunk_plan(const cb_config* cfg, int32_t batch, const int32_t* kv_l
   const ChunkPlan p = plan_chunk(*cfg, ws_layout(*cfg), splits, tile_rows, batch, kv_len, token_offsets);
   plan[0] = p.tile_rows;
   plan[1] = p.nsplit;
-  plan[2] = p.chunk;
+  plan[2] = p.splits.keys[0];
   plan[3] = (int32_t)std::min<int64_t>(p.jobs, INT32_MAX);
   plan[4] = p.tiles;
   return CB_OK;

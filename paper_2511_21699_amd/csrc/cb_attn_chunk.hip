@@ -914,42 +914,86 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
   return false;
 }
 
+// The split merge by the last workgroup of a tile to arrive (split_merge's, for tiles whose row tiles are a wavefront's each): a wavefront
+// has a row tile's whole states of two splits under way at once, where a few pieces at a time are a round trip to memory each (tiles of 128 rows
+// in two splits: 8 us at the end of a workgroup).  The splits are added up in their order, whoever arrives last.
+template <int D>
+__device__ __forceinline__ void merge_by_last(const AttnParams& p, const TileJob& jb, int* flag_lds) {
+  constexpr int P = PartialLayout<D, 32, true>::P;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
+  CB_GLOBAL unsigned long long* const ticket = (CB_GLOBAL unsigned long long*)p.tickets + 2 * (((int64_t)jb.b * p.Hkv + jb.hk) * jb.tiles + jb.rt);
+  const unsigned long long xcc = __builtin_amdgcn_s_getreg(20 | (0 << 6) | ((4 - 1) << 11)) & 15u;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) {
+    const unsigned long long arrive = 1ull | (xcc << 24) | ((xcc * xcc) << 40);
+    const unsigned long long tot = __hip_atomic_fetch_add(ticket, arrive, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + arrive, n = tot & 0xfffull;
+    int flag = n == (unsigned long long)jb.nsplit ? 1 : 0;
+    if (flag) {
+      if (((tot >> 24) & 0xffffull) != n * xcc || tot >> 40 != n * xcc * xcc) flag = 2;  // (some split ran on another XCD: not in this L2)
+      __hip_atomic_store(ticket, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // ready for the next launch
+    }
+    *flag_lds = flag;
+  }
+  __syncthreads();
+  const int flag = *flag_lds;
+  if (!flag) return;
+  const __amdgpu_buffer_rsrc_t prsrc = partial_rsrc<D, 32, true>(p, jb);
+  const int rows = jb.M - jb.row0 < p.tile_rows ? jb.M - jb.row0 : p.tile_rows;
+  for (int i = w; i * 32 < rows; i += kWideWaves) {
+    const int row = jb.row0 + i * 32 + (l & 31), token = row / jb.g;
+    const int64_t gr = row < jb.M ? (int64_t)(jb.off + token) * p.Hq + jb.hk * jb.g + (row - token * jb.g) : -1;
+    const uint32_t byte = partial_byte<D, 32, true>(p, jb, i);
+    if (flag == 1) merge_pieces<D, 32, true, P, 0, 2>(prsrc, gr, byte, (CB_GLOBAL uint16_t*)p.out, jb.nsplit, 0, l);
+    else merge_pieces<D, 32, true, P, kAgentCoherent, 2>(prsrc, gr, byte, (CB_GLOBAL uint16_t*)p.out, jb.nsplit, 0, l);
+  }
+}
+
 template <int D, bool PG>
-__global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_few(AttnParams p_arg, SeqMeta meta) {
+__global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_few(AttnParams p_arg, SeqMeta meta, ChunkSplits splits) {
   const SeqMetaLanes ml = seq_meta_prefetch(meta);
+  const int lane_chunk = splits.keys[threadIdx.x & 63];
   __shared__ __align__(1024) uint4 ring[Feed<D, kWideWaves, 32>::kRingVecs];
   __shared__ TileLds sh;
   AttnParams p = p_arg;
   pin_args(p);
   TileJob jb;
-  if (!chunk_job(p, ml, blockIdx.x, jb)) return;
+  if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
   if (sweep_chunk<D, PG, 1, 2, false>(p, jb, sh, ring)) sweep_chunk<D, PG, 1, 2, true>(p, jb, sh, ring);
   if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
 }
 
 template <int D, bool PG>
-__global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_tall(AttnParams p_arg, SeqMeta meta) {
+__global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_tall(AttnParams p_arg, SeqMeta meta, ChunkSplits splits) {
   const SeqMetaLanes ml = seq_meta_prefetch(meta);
+  const int lane_chunk = splits.keys[threadIdx.x & 63];
   __shared__ __align__(1024) uint4 ring[Feed<D, kWideWaves, 32>::kRingVecs];
   __shared__ TileLds sh;
   AttnParams p = p_arg;
   pin_args(p);
   TileJob jb;
-  if (!chunk_job(p, ml, blockIdx.x, jb)) return;
+  if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
   sweep_tall<D, PG>(p, jb, sh, ring);
-  if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 256, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
+  if (jb.nsplit == 1) return;
+  if (p.coop_merge) split_merge<D, 32, true, kWideWaves, 256, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
+  else merge_by_last<D>(p, jb, &sh.flag);
 }
 
 template <int D, bool PG>
-__global__ __launch_bounds__(64 * kWideWaves, 2) void k_chunk_many(AttnParams p_arg, SeqMeta meta) {
+__global__ __launch_bounds__(64 * kWideWaves, 2) void k_chunk_many(AttnParams p_arg, SeqMeta meta, ChunkSplits splits) {
   const SeqMetaLanes ml = seq_meta_prefetch(meta);
+  const int lane_chunk = splits.keys[threadIdx.x & 63];
   __shared__ __align__(1024) ManyLds<D> sh;
   AttnParams p = p_arg;
   pin_args(p);
   TileJob jb;
-  if (!chunk_job(p, ml, blockIdx.x, jb)) return;
+  if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
   if (sweep_many<D, PG, false>(p, jb, sh)) sweep_many<D, PG, true>(p, jb, sh);
   if (jb.nsplit == 1) return;
+  if (!p.coop_merge) {
+    merge_by_last<D>(p, jb, &sh.flag);
+    return;
+  }
   __syncthreads();  // (everybody is done with the rings, whose place the merge's words take)
   static_assert(sizeof(TileLds) <= sizeof(sh.ring), "");
   split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, *reinterpret_cast<TileLds*>(sh.ring), nullptr, [] {});
@@ -961,19 +1005,19 @@ int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch) {
 }
 
 template <int D>
-static hipError_t launch_dim(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs) {
+static hipError_t launch_dim(hipStream_t st, const AttnParams& p, const SeqMeta& meta, const ChunkSplits& splits, int wgs) {
   const dim3 grid(wgs), block(64 * kWideWaves);
   const bool paged = p.kv.block_size > 0;
-  if (p.tile_rows == 64 && paged) hipLaunchKernelGGL((k_chunk_few<D, true>), grid, block, 0, st, p, meta);
-  else if (p.tile_rows == 64) hipLaunchKernelGGL((k_chunk_few<D, false>), grid, block, 0, st, p, meta);
-  else if (p.tile_rows == 128 && paged) hipLaunchKernelGGL((k_chunk_many<D, true>), grid, block, 0, st, p, meta);
-  else if (p.tile_rows == 128) hipLaunchKernelGGL((k_chunk_many<D, false>), grid, block, 0, st, p, meta);
-  else if (paged) hipLaunchKernelGGL((k_chunk_tall<D, true>), grid, block, 0, st, p, meta);
-  else hipLaunchKernelGGL((k_chunk_tall<D, false>), grid, block, 0, st, p, meta);
+  if (p.tile_rows == 64 && paged) hipLaunchKernelGGL((k_chunk_few<D, true>), grid, block, 0, st, p, meta, splits);
+  else if (p.tile_rows == 64) hipLaunchKernelGGL((k_chunk_few<D, false>), grid, block, 0, st, p, meta, splits);
+  else if (p.tile_rows == 128 && paged) hipLaunchKernelGGL((k_chunk_many<D, true>), grid, block, 0, st, p, meta, splits);
+  else if (p.tile_rows == 128) hipLaunchKernelGGL((k_chunk_many<D, false>), grid, block, 0, st, p, meta, splits);
+  else if (paged) hipLaunchKernelGGL((k_chunk_tall<D, true>), grid, block, 0, st, p, meta, splits);
+  else hipLaunchKernelGGL((k_chunk_tall<D, false>), grid, block, 0, st, p, meta, splits);
   return hipGetLastError();
 }
-hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs) {
-  return p.D == 64 ? launch_dim<64>(st, p, meta, wgs) : launch_dim<128>(st, p, meta, wgs);
+hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, const ChunkSplits& splits, int wgs) {
+  return p.D == 64 ? launch_dim<64>(st, p, meta, splits, wgs) : launch_dim<128>(st, p, meta, splits, wgs);
 }
 
 }  // namespace cb

@@ -50,13 +50,14 @@ __device__ __forceinline__ float state_weight(float m, float ref) { return m == 
 __device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
 template <int D, int RT>
-__global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_chunk_f32(AttnParams p, SeqMeta meta) {
+__global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_chunk_f32(AttnParams p, SeqMeta meta, ChunkSplits splits) {
   constexpr int NJ = D / 16, NB = D / 64, ROWS = 16 * RT;
   __shared__ ChunkF32Lds<D, RT> sh;
   const SeqMetaLanes ml = seq_meta_prefetch(meta);
+  const int lane_chunk = splits.keys[threadIdx.x & 63];
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, r = l & 15, h = l >> 4;
   TileJob jb;
-  if (!chunk_job(p, ml, blockIdx.x, jb)) return;
+  if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
   const int b = jb.b, hk = jb.hk, k0 = jb.k0, k1 = jb.k1, nsplit = jb.nsplit, nu = (k1 - k0 + kF32Unit - 1) / kF32Unit;
   const int S = jb.S + jb.row0 / jb.g + 1;  // (every row sees the keys below)
   const CBL_GLOBAL float* const kb = (const CBL_GLOBAL float*)p.kv.k;
@@ -286,12 +287,12 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_
   }
 }
 
-hipError_t launch_attn_chunk_f32(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs) {
+hipError_t launch_attn_chunk_f32(hipStream_t st, const AttnParams& p, const SeqMeta& meta, const ChunkSplits& splits, int wgs) {
   const dim3 grid(wgs), block(64 * kF32Waves);
-  if (p.D == 64 && p.tile_rows == 16) hipLaunchKernelGGL((k_chunk_f32<64, 1>), grid, block, 0, st, p, meta);
-  else if (p.D == 64) hipLaunchKernelGGL((k_chunk_f32<64, 2>), grid, block, 0, st, p, meta);
-  else if (p.tile_rows == 16) hipLaunchKernelGGL((k_chunk_f32<128, 1>), grid, block, 0, st, p, meta);
-  else hipLaunchKernelGGL((k_chunk_f32<128, 2>), grid, block, 0, st, p, meta);
+  if (p.D == 64 && p.tile_rows == 16) hipLaunchKernelGGL((k_chunk_f32<64, 1>), grid, block, 0, st, p, meta, splits);
+  else if (p.D == 64) hipLaunchKernelGGL((k_chunk_f32<64, 2>), grid, block, 0, st, p, meta, splits);
+  else if (p.tile_rows == 16) hipLaunchKernelGGL((k_chunk_f32<128, 1>), grid, block, 0, st, p, meta, splits);
+  else hipLaunchKernelGGL((k_chunk_f32<128, 2>), grid, block, 0, st, p, meta, splits);
   return hipGetLastError();
 }
 

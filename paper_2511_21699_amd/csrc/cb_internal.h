@@ -293,10 +293,14 @@ struct ChunkArgs {
   float scale;
 };
 hipError_t launch_chunk_rows(hipStream_t st, const ChunkArgs& a, const SeqMeta& meta, int dtype, int D);
+// Keys per split of every sequence: jobs of about one length, whatever the sequences' are.
+struct ChunkSplits {
+  int32_t keys[CB_MAX_BATCH];
+};
 // bf16 on the matrix cores, blocks of a power of two (cb_attn_chunk.hip): grid_y = row tiles of the longest chunk per kv head, meta.start =
 // workgroups in front of each sequence's, in the order of meta.by_length
-hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs);
-hipError_t launch_attn_chunk_f32(hipStream_t st, const AttnParams& p, const SeqMeta& meta, int wgs);
+hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, const ChunkSplits& splits, int wgs);
+hipError_t launch_attn_chunk_f32(hipStream_t st, const AttnParams& p, const SeqMeta& meta, const ChunkSplits& splits, int wgs);
 int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch);  // of one split
 
 // Log probabilities (cb_logprob.hip).  The parts of a row, where there are several: a state of kLpHeader + top_k 64-bit words each in the
@@ -339,8 +343,8 @@ extern "C" int cb_debug_layers(const cb_config* cfg, int32_t layers, int32_t bat
 extern "C" int cb_debug_step(cb_ctx* ctx, int32_t info[4]);
 // The pool size that the kernels clamp the block table's entries to (0: contiguous, -1: unknown layout).
 extern "C" int64_t cb_debug_pool_blocks(const cb_config* cfg, const cb_kv_layer* layer);
-// How a chunk's attention is cut up (splits, tile_rows: the options, 0 = automatic): plan[0] = rows of a tile, [1] = splits of the longest, [2] = keys per split,
-// [3] = workgroups, [4] = row tiles of the longest chunk per kv head
+// How a chunk's attention is cut up (splits, tile_rows: the options, 0 = automatic): plan[0] = rows of a tile, [1] = splits of the longest, [2] = keys per split of the first
+// sequence, [3] = workgroups, [4] = row tiles of the longest chunk per kv head
 extern "C" int cb_debug_chunk_plan(const cb_config* cfg, int32_t batch, const int32_t* kv_len, const int32_t* token_offsets, int32_t splits, int32_t tile_rows, int32_t plan[5]);
 // The argument checks of the calls around the verification (err: 256 bytes).
 extern "C" int cb_debug_check_append(const cb_config* cfg, int32_t batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,

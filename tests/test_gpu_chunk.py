@@ -61,6 +61,43 @@ def test_chunk_attention_against_64_bits(i):
     assert torch.equal(again, out[:b.n])
 
 
+TILES = [  # the kernels and their split merges, whatever the planner would take: dtype, heads, kv heads, head_dim, prefixes, new tokens, block
+    ("bf16", 8, 2, 128, [95, 0, 700], [70, 200, 3], 16),
+    ("bf16", 6, 6, 128, [33], [530], 0),
+    ("bf16", 10, 2, 64, [0, 1111], [150, 1], 1),
+    ("bf16", 4, 4, 64, [64], [400], 0),
+    ("f32", 8, 2, 128, [95, 0, 300], [20, 60, 1], 16),
+    ("f32", 6, 3, 64, [10], [90], 0),
+]
+
+
+@pytest.mark.parametrize("case", TILES)
+@pytest.mark.parametrize("rows", [64, 128, 256])
+@pytest.mark.parametrize("splits, coop", [(1, 1), (2, 1), (3, 0), (7, 1), (8, 0)])
+def test_every_tile_and_split(case, rows, splits, coop):
+    import torch
+    print(f"[case] tiles {case} {rows} {splits} {coop}", flush=True)
+    dtype, hq, hkv, d, lens, new, block = case
+    b = Batch(dtype, hq, hkv, d, lens, new, block, seed=rows + splits, scale=2.0)
+    for name, value in (("tile_rows", rows), ("splits", splits), ("coop_merge", coop)):
+        b.ver.set_option(name, value)
+    out = torch.full((b.n + 1, hq, d), 55.0, dtype=b.t, device="cuda")
+    for _ in range(2):
+        b.ver.chunk_attention(b.q, b.kv, b.kv_len, b.off, out)
+        torch.cuda.synchronize()
+        _check(b, out)
+        assert (out[b.n:] == 55.0).all()
+        out[:b.n] = 0
+    t = new[0] - 1  # the first sequence's last token holds anything: nobody else sees it
+    clean = b.ver.chunk_attention(b.q, b.kv, b.kv_len, b.off)
+    if t > 0:
+        b.put(0, int(lens[0]) + t, torch.full((1, hkv, d), float("nan"), dtype=b.t, device="cuda"), torch.full((1, hkv, d), float("inf"), dtype=b.t, device="cuda"))
+        odd = b.ver.chunk_attention(b.q, b.kv, b.kv_len, b.off)
+        torch.cuda.synchronize()
+        assert torch.equal(odd[:t], clean[:t]) and torch.equal(odd[t + 1:], clean[t + 1:])
+        assert odd[t].isnan().all()
+
+
 @pytest.mark.parametrize("dtype, d, hq, hkv, s, n", [("bf16", 128, 8, 2, 20, 90), ("bf16", 64, 4, 4, 3, 300), ("f32", 128, 4, 2, 40, 50), ("bf16", 128, 4, 4, 600, 40)])
 @pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
 def test_what_a_token_must_not_see_can_hold_anything(dtype, d, hq, hkv, s, n, what):
