@@ -1,5 +1,6 @@
 // Host side of libcacheback_verify.so: argument checks, workspace layout, launch planning and the
 // extern "C" entry points declared in cacheback.h.  No arithmetic of the method happens here.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -1093,8 +1094,10 @@ struct ChunkPlan {
 // The cheapest of a few plans by an estimate of the launch's time, in us.  A sequence is cut into as many equal splits as its length has of the
 // longest's, so that jobs are of about one length.  A job takes `start` beside its sweep and `alone` for every 32 keys where it has a compute
 // unit for itself; a compute unit gets through 32 keys of a tile in `full`, with as many workgroups as it holds, at the clock of a busy chip.  The longest
-// are dispatched first, so the launch ends with the longest job or, where there are more than compute units, when the work is shared out and a job of
-// the shortest is through; nor before the cache has been read.  Splits have the room that the workspace has.
+// are dispatched first (chunk_job), so a launch ends with its longest job or, where there are more jobs than places, when the work is shared out
+// and what is left of a round of the shortest is through.  Reading the cache takes its time beside that, and both slow each other down where they are
+// about as long: more where one workgroup after the other has a compute unit, as then the long jobs of matrix products come first and the short ones
+// of single tokens, which read, last.  Splits have the room that the workspace has.
 ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, int opt_tile_rows, int batch, const int32_t* kv_len, const int32_t* off) {
   const bool f32 = c.qkv_dtype == CB_F32;
   const int g = c.num_q_heads / c.num_kv_heads, Hkv = c.num_kv_heads;
@@ -1107,7 +1110,7 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     len_max = std::max(len_max, kv_len[b] + n);
     slots += kv_len[b] + n;
   }
-  const double memory = slots * Hkv * c.head_dim * (f32 ? 8 : 4) / 4.6e6 + 3.0, by_dim = c.head_dim == 128 ? 1.0 : 0.6;
+  const double memory = slots * Hkv * c.head_dim * (f32 ? 8 : 4) / 4.6e6 + 3.0;
   const int64_t m_max = (int64_t)n_max * g, total = off[batch];
   // A split's partial states, and tiles that there are tickets for.  (Within a sequence the bf16 kernel's offsets have 31 bits.)
   const int64_t per_split = f32 ? total * c.num_q_heads * partial_stride(c.head_dim) * 4 : chunk_partial_bytes(c.head_dim, total, c.num_q_heads, Hkv, batch);
@@ -1115,18 +1118,23 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
   const int64_t most_here = f32 ? INT32_MAX : ((1ll << 31) - 1) / chunk_partial_bytes(c.head_dim, n_max, c.num_q_heads, Hkv, 2);
   struct Tile {
     int rows;
-    double alone, full, start, merge;
+    double alone, full, start, merge, coop;  // coop: a merge in a launch that is resident at once
+    double dim64;                            // alone and full at head_dim 64
   };
-  // (4096 to 8192 tokens, and 256 behind 30000, 32/8 heads; the fp32 ones 512 behind 4096)
-  static const Tile kBf16[] = {{64, 0.36, 0.36, 4.0, 2.0}, {128, 0.66, 0.52, 5.0, 3.0}, {256, 0.86, 0.96, 7.0, 5.0}};
-  static const Tile kF32[] = {{16, 0.43, 0.43, 3.0, 2.5}, {32, 0.8, 0.8, 4.0, 3.0}};
+  // From launches of 1 to 8192 tokens of 32/8 and 32/32 heads over up to 65536 keys.  With tiles of 64, 128 and 256 rows 8192 tokens from the first take
+  // 730, 533 and 543 us, 4096 behind 28672 3089, 2102 and 1901, 256 behind 30000 in one split 387, 569 and 777, in eight 240, 156 and 131.
+  static const Tile kBf16[] = {{64, 0.36, 0.36, 6.0, 2.0, 2.5, 0.78}, {128, 0.66, 0.52, 4.5, 2.5, 5.0, 0.7}, {256, 0.86, 0.96, 8.0, 4.0, 10.0, 1.0}};
+  static const Tile kF32[] = {{16, 0.43, 0.43, 3.0, 1.0, 2.5, 0.6}, {32, 0.8, 0.8, 4.0, 1.0, 3.0, 0.6}};
   ChunkPlan best{};
   double best_us = 0;
-  for (int kind = 0; kind < (f32 ? 2 : 3); kind++) {
+  for (int kind = 0; kind < (f32 || c.head_dim == 64 ? 2 : 3); kind++) {
     const Tile& tile = f32 ? kF32[kind] : kBf16[kind];
     const int rows = tile.rows;
-    if (opt_tile_rows && !f32 ? rows != opt_tile_rows : best.jobs && m_max <= rows / 2) continue;
-    const double alone = tile.alone * by_dim, full = tile.full * by_dim, start = tile.start;
+    if (opt_tile_rows && !f32 ? rows != std::min(opt_tile_rows, c.head_dim == 64 ? 128 : 256) : best.jobs && m_max <= rows / 2) continue;
+    const double by_dim = c.head_dim == 64 ? tile.dim64 : 1.0, alone = tile.alone * by_dim, full = tile.full * by_dim, start = tile.start;
+    const bool two = rows == 128 && !f32;  // (workgroups to a compute unit, whose starts and tails hide behind each other)
+    // (the tallest tiles take units that some query does not see whole 1.5 times longer)
+    const double masks = rows == 256 ? 1.5 * rows / g / 32 : 0.0;
     const int tiles_max = (int)((m_max + rows - 1) / rows);
     int64_t tiles = 0;
     for (int b = 0; b < batch; b++) tiles += ((int64_t)(off[b + 1] - off[b]) * g + rows - 1) / rows * Hkv;
@@ -1150,7 +1158,7 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
         p.nsplit = std::max(p.nsplit, ns_b);
         p.jobs += (int64_t)nt * Hkv * ns_b;
         if (ns_b == 1) {  // (whole tiles: their lengths are evenly spaced)
-          const double first = (s + std::min(n, (rows + g - 1) / g) + 31) / 32, end = (len + 31) / 32;
+          const double first = (s + std::min(n, (rows + g - 1) / g) + 31) / 32 + masks, end = (len + 31) / 32 + masks;
           work += 0.5 * (first + end) * nt * Hkv;
           longest = std::max(longest, end);
           shortest = std::min(shortest, first);
@@ -1166,11 +1174,13 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
           merged += whole + (rest > 0) > 1 ? Hkv : 0;
         }
       }
-      const double merge = p.nsplit == 1 ? 0.0 : real <= 256 ? 1.5 : tile.merge + 0.15 * p.nsplit;
-      const double one = longest * alone + start + merge;
-      const bool two = rows == 128 && !f32;  // (workgroups to a compute unit, whose starts and tails hide behind each other)
-      const double shared = (work * full + real * (two ? 0.3 : 1.0) * start + merged * merge * (two ? 0.5 : 1.0)) / 256 + shortest * full + (two ? start : 0.0);
-      const double us = std::max(memory + merge, real <= 256 ? one : std::max(one, shared));
+      const double merge = p.nsplit == 1 ? 0.0 : p.jobs <= 256 ? tile.coop : tile.merge * std::min(p.nsplit + 1, 8);
+      const double places = two ? 512.0 : 256.0, one = longest * alone + start * (p.jobs > places ? 2 : 1) + merge, rounds = std::ceil(real / places) - real / places;
+      double shared = (work * full + real * (two ? 0.3 : 1.0) * start + merged * merge) / 256 + rounds * shortest * full;
+      if (two && real <= 512) shared = std::max((work * full + merged * merge) / 256, (longest + shortest) * full);
+      if (two) shared += start;
+      const double sweep = real <= 256 ? one : std::max(one, shared), s2 = sweep * sweep, m2 = memory * memory;
+      const double us = real > 256 && !two ? std::sqrt(s2 + m2) : std::sqrt(std::sqrt(s2 * s2 + m2 * m2));
       if (best.jobs == 0 || us < best_us * 0.99 - 0.1) {
         best = p;
         best_us = us;

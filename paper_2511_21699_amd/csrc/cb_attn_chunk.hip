@@ -1012,8 +1012,9 @@ static hipError_t launch_dim(hipStream_t st, const AttnParams& p, const SeqMeta&
   else if (p.tile_rows == 64) hipLaunchKernelGGL((k_chunk_few<D, false>), grid, block, 0, st, p, meta, splits);
   else if (p.tile_rows == 128 && paged) hipLaunchKernelGGL((k_chunk_many<D, true>), grid, block, 0, st, p, meta, splits);
   else if (p.tile_rows == 128) hipLaunchKernelGGL((k_chunk_many<D, false>), grid, block, 0, st, p, meta, splits);
-  else if (paged) hipLaunchKernelGGL((k_chunk_tall<D, true>), grid, block, 0, st, p, meta, splits);
-  else hipLaunchKernelGGL((k_chunk_tall<D, false>), grid, block, 0, st, p, meta, splits);
+  else if (D == 64) return hipErrorInvalidValue;  // (4096 tokens, 32/8 heads: 118 us, with tiles of 128 rows 97)
+  else if (paged) hipLaunchKernelGGL((k_chunk_tall<128, true>), grid, block, 0, st, p, meta, splits);
+  else hipLaunchKernelGGL((k_chunk_tall<128, false>), grid, block, 0, st, p, meta, splits);
   return hipGetLastError();
 }
 hipError_t launch_attn_chunk(hipStream_t st, const AttnParams& p, const SeqMeta& meta, const ChunkSplits& splits, int wgs) {
