@@ -198,7 +198,7 @@ def scratch_violations(asm: str, file_name: str = "") -> list:
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")))
-    checked = ["cb_attn_wide_px.hip", "cb_attn_wide.hip", "cb_attn_wide_layers.hip", "cb_attn_wide_step.hip", "cb_attn_mfma.hip", "cb_attn_chunk.hip"]
+    checked = ["cb_attn_wide_px.hip", "cb_attn_wide.hip", "cb_attn_wide_layers.hip", "cb_attn_wide_step.hip", "cb_attn_mfma.hip", "cb_attn_chunk.hip", "cb_attn_chunk_f32.hip"]
     with ThreadPoolExecutor(max_workers=min(8, len(srcs) + len(checked))) as ex:
         listings = [ex.submit(device_asm, os.path.join(CSRC, name)) for name in checked]  # (the longest first, beside the compilation)
         objs = list(ex.map(_compile, sorted(srcs, key=lambda s: os.path.basename(s) not in checked)))

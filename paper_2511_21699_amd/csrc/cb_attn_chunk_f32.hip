@@ -6,14 +6,18 @@
 // A workgroup of 8 wavefronts has RT row tiles of 16 rows of a kv head and a split of their keys.  The wavefronts take units of 16 keys in turn
 // and share nothing until the end: K and V go straight from memory to the registers that the MFMAs read, and serve RT tiles.  The
 // wavefronts' states are combined through LDS, the splits' by the tile's last workgroup.
-// What bounds it: a unit is RT D / 2 MFMAs of 32 cycles, two wavefronts to a SIMD, against D * 128 bytes per wavefront from the L2 -- 32 of the 64
-// bytes a clock that a compute unit can take with one row tile, 16 with two.
+// What bounds it: prompts the matrix cores, a unit is RT D / 2 MFMAs of 32 cycles with two wavefronts to a SIMD (heads of 128, two row tiles: busy 63%
+// of the time at 2.16 GHz, waiting for V most of the rest; 32/8 heads, 512 tokens behind 4096 in 388 us, 94 TFLOP/s).  Single tokens the loads on their way:
+// a compute unit takes 39 bytes a ns.  One token behind 8192 25 us, 16 behind 2000 each 57 us (4.6 TB/s); with a table's entries asked for
+// where they are needed, V not ahead and eight splits at a time in the merge these were 40 and 78.
 //
 // Register layouts (lane l, r = l % 16, h = l / 16):
 //   scores transposed, S^T = K Q^T: MFMA (j, e) contracts the dims 16j + 4h + e; A = K[key r], B = Q[query r], so both
 //   are 16-byte pieces of a row, and D[v] = S^T[key 4h+v][query r].
 //   O^T = V^T P^T: MFMA (v, n, e) contracts the keys 4h + v; B = the lane's own probability v, A = V[key 4h+v][dim
 //   64n + 4r + e], again 16-byte pieces; D[i] = O^T[dim 64n + 16h + 4i + e][query r].
+#include <type_traits>
+
 #include "cb_chunk.h"
 
 namespace cb {
@@ -74,26 +78,47 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_
 #pragma unroll
     for (int j = 0; j < NJ; j++) q[t][j] = qp[4 * j + h];
   }
-  // keys past the split's end repeat its last one (masked below), so every address stays inside the sequence
-  auto load_k = [&](int u, f32x4 (&k)[NJ]) {
+  // Where lane l's key of a unit (r) is.  The table's entry is asked for two units ahead and becomes an offset one ahead, so that no load waits for
+  // another one's address.  Keys past the split's end repeat its last one (masked below): every address stays inside the sequence.
+  auto look_up = [&](int u, int& block, int& slot) {
     int key = k0 + u * kF32Unit + r;
     key = key < k1 ? key : k1 - 1;
-    const CBL_GLOBAL f32x4* const kp = (const CBL_GLOBAL f32x4*)(kb + slot_offset(p.kv, b, key, hk));
+    block = b;
+    slot = key;
+    if (p.kv.block_size > 0) {
+      const int lb = key / p.kv.block_size;
+      slot = key - lb * p.kv.block_size;
+      block = as_global(p.kv.block_table)[(int64_t)b * p.kv.max_blocks + lb];
+    }
+  };
+  auto place = [&](int block, int slot) {
+    if (p.kv.block_size > 0) block = block < 0 ? 0 : block >= p.kv.num_blocks ? (int)p.kv.num_blocks - 1 : block;
+    return block * p.kv.seq_stride + slot * p.kv.token_stride + hk * p.kv.head_stride;
+  };
+  auto load_k = [&](int64_t off, f32x4 (&k)[NJ]) {
+    const CBL_GLOBAL f32x4* const kp = (const CBL_GLOBAL f32x4*)(kb + off);
 #pragma unroll
     for (int j = 0; j < NJ; j++) k[j] = kp[4 * j + h];
   };
-  auto load_v = [&](int u, f32x4 (&v)[4][NB]) {
+  auto load_v = [&](int64_t off, f32x4 (&v)[4][NB]) {
 #pragma unroll
     for (int x = 0; x < 4; x++) {
-      int key = k0 + u * kF32Unit + 4 * h + x;
-      key = key < k1 ? key : k1 - 1;
-      const CBL_GLOBAL f32x4* const vp = (const CBL_GLOBAL f32x4*)(vb + slot_offset(p.kv, b, key, hk));
+      const uint32_t lo = __builtin_amdgcn_ds_bpermute(4 * (4 * h + x), (int)(uint32_t)off), hi = __builtin_amdgcn_ds_bpermute(4 * (4 * h + x), (int)(off >> 32));
+      const CBL_GLOBAL f32x4* const vp = (const CBL_GLOBAL f32x4*)(vb + (int64_t)(((uint64_t)hi << 32) | lo));
 #pragma unroll
       for (int n = 0; n < NB; n++) v[x][n] = vp[16 * n + r];
     }
   };
-  f32x4 k[NJ];
-  load_k(w, k);
+  // K and V are asked for a unit ahead where there are registers for it: V with one row tile, K unless heads of 64 have four wavefronts to a SIMD
+  // (then its loads go out when the scores are through with the registers).
+  constexpr bool K_AHEAD = RT == 2 || D == 128, V_AHEAD = RT == 1;
+  f32x4 k[NJ], v[4][NB];
+  int block, slot;
+  look_up(w, block, slot);
+  int64_t off = place(block, slot);
+  load_k(off, k);
+  if (V_AHEAD) load_v(off, v);
+  look_up(w + kF32Waves, block, slot);
   f32x4 o[RT][NB][4];
   float m[RT], lsum[RT];
 #pragma unroll
@@ -106,9 +131,12 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_
     lsum[t] = 0.f;
   }
   for (int u = w; u < nu; u += kF32Waves) {
-    f32x4 v[4][NB], kn[NJ];
-    load_v(u, v);
-    load_k(u + kF32Waves, kn);
+    f32x4 kn[NJ], vn[4][NB];
+    const int64_t next = place(block, slot);
+    look_up(u + 2 * kF32Waves, block, slot);
+    load_v(V_AHEAD ? next : off, V_AHEAD ? vn : v);
+    if (K_AHEAD) load_k(next, kn);
+    off = next;
     f32x4 s[RT], s1[RT];
 #pragma unroll
     for (int t = 0; t < RT; t++) s[t] = s1[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -121,6 +149,7 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_
           s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][e], q[t][j][e], s[t], 0, 0, 0);
           s1[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j + 1][e], q[t][j + 1][e], s1[t], 0, 0, 0);
         }
+    if (!K_AHEAD) load_k(next, k);
     const int key0 = k0 + u * kF32Unit;
     const bool masked = key0 + kF32Unit > (S < k1 ? S : k1);  // (uniform)
     bool odd_v = false;
@@ -172,24 +201,34 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_
           for (int t = 0; t < RT; t++) o[t][n][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[x][n][e], pr[t][x], o[t][n][e], 0, 0, 0);
     if (__builtin_expect(odd_v, 0)) {  // infinities or NaN among the unit's values, for the queries that do see them
 #pragma unroll
-      for (int t = 0; t < RT; t++)
-        for (int kk = 0; kk < kF32Unit && key0 + kk < k1; kk++) {
-          const float mine = (kk & 2) ? ((kk & 1) ? pr[t][3] : pr[t][2]) : ((kk & 1) ? pr[t][1] : pr[t][0]);
-          const float pk = __shfl(mine, (kk >> 2) * 16 + r, 64);
-          const CBL_GLOBAL float* const vp = vb + slot_offset(p.kv, b, key0 + kk, hk);
+      for (int x = 0; x < 4; x++)
+        for (int part = 0; part < 4 && key0 + 4 * part + x < k1; part++) {
+          const CBL_GLOBAL float* const vp = vb + slot_offset(p.kv, b, key0 + 4 * part + x, hk);
 #pragma unroll
-          for (int n = 0; n < NB; n++)
+          for (int t = 0; t < RT; t++) {
+            const float pk = __shfl(pr[t][x], 16 * part + r, 64);
 #pragma unroll
-            for (int e = 0; e < 4; e++)
+            for (int n = 0; n < NB; n++)
 #pragma unroll
-              for (int i = 0; i < 4; i++) {
-                const float x = vp[64 * n + 16 * h + 4 * i + e];
-                o[t][n][e][i] += (is_finite(x) || pk == 0.f) ? 0.f : pk * x;
-              }
+              for (int e = 0; e < 4; e++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                  const float odd = vp[64 * n + 16 * h + 4 * i + e];
+                  o[t][n][e][i] += (is_finite(odd) || pk == 0.f) ? 0.f : pk * odd;
+                }
+          }
         }
     }
+    if (V_AHEAD) {
 #pragma unroll
-    for (int j = 0; j < NJ; j++) k[j] = kn[j];
+      for (int x = 0; x < 4; x++)
+#pragma unroll
+        for (int n = 0; n < NB; n++) v[x][n] = vn[x][n];
+    }
+    if (K_AHEAD) {
+#pragma unroll
+      for (int j = 0; j < NJ; j++) k[j] = kn[j];
+    }
   }
 
   // The wavefronts' states into one.  Thread t then owns 4 dims of a row.
@@ -251,40 +290,46 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_
   }
   __syncthreads();
   if (!sh.last) return;
-  constexpr int BS = 8;   // splits whose loads are in flight together
+  auto merge = [&](auto batch) {   // (splits whose loads are in flight together)
+    constexpr int BS = decltype(batch)::value;
 #pragma unroll
-  for (int i = 0; i < N; i++) {
-    if (!live(i)) continue;
-    const int64_t grow = out_row(i);
-    const float* const part = p.partial + grow * p.nsplit * PS;
-    float mm = -INFINITY, ll = 0.f;
-    f32x4 oo = {0.f, 0.f, 0.f, 0.f};
-    for (int t0 = 0; t0 < nsplit; t0 += BS) {
-      float2 st[BS], x0[BS], x1[BS];
+    for (int i = 0; i < N; i++) {
+      if (!live(i)) continue;
+      const int64_t grow = out_row(i);
+      const float* const part = p.partial + grow * p.nsplit * PS;
+      float mm = -INFINITY, ll = 0.f;
+      f32x4 oo = {0.f, 0.f, 0.f, 0.f};
+      for (int t0 = 0; t0 < nsplit; t0 += BS) {
+        float2 st[BS], x0[BS], x1[BS];
 #pragma unroll
-      for (int x = 0; x < BS; x++) {
-        const float* const pp = part + (t0 + x < nsplit ? t0 + x : nsplit - 1) * PS;
-        st[x] = get_pair(pp + D);
-        x0[x] = get_pair(pp + c);
-        x1[x] = get_pair(pp + c + 2);
+        for (int x = 0; x < BS; x++) {
+          const float* const pp = part + (t0 + x < nsplit ? t0 + x : nsplit - 1) * PS;
+          st[x] = get_pair(pp + D);
+          x0[x] = get_pair(pp + c);
+          x1[x] = get_pair(pp + c + 2);
+        }
+        float mn = mm;
+#pragma unroll
+        for (int x = 0; x < BS; x++) mn = fmaxf(mn, st[x].x);
+        const float alpha = state_weight(mm, mn);
+        oo *= alpha;
+        ll *= alpha;
+        mm = mn;
+#pragma unroll
+        for (int x = 0; x < BS; x++) {
+          const bool more = t0 + x < nsplit;   // (not the last one once more)
+          const float wgt = state_weight(st[x].x, mm);
+          ll = more ? ll + st[x].y * wgt : ll;
+          const f32x4 sum = oo + f32x4{x0[x].x, x0[x].y, x1[x].x, x1[x].y} * wgt;
+#pragma unroll
+          for (int e = 0; e < 4; e++) oo[e] = more ? sum[e] : oo[e];
+        }
       }
-      float mn = mm;
-#pragma unroll
-      for (int x = 0; x < BS; x++) mn = fmaxf(mn, st[x].x);
-      const float alpha = state_weight(mm, mn);
-      oo *= alpha;
-      ll *= alpha;
-      mm = mn;
-#pragma unroll
-      for (int x = 0; x < BS; x++) {
-        if (t0 + x >= nsplit) break;  // (a repeated split)
-        const float wgt = state_weight(st[x].x, mm);
-        ll += st[x].y * wgt;
-        oo += f32x4{x0[x].x, x0[x].y, x1[x].x, x1[x].y} * wgt;
-      }
+      *(CBL_GLOBAL f32x4*)((CBL_GLOBAL float*)p.out + grow * D + c) = oo / ll;
     }
-    *(CBL_GLOBAL f32x4*)((CBL_GLOBAL float*)p.out + grow * D + c) = oo / ll;
-  }
+  };
+  if (nsplit <= 8) merge(std::integral_constant<int, 8>{});
+  else merge(std::integral_constant<int, 16>{});
 }
 
 hipError_t launch_attn_chunk_f32(hipStream_t st, const AttnParams& p, const SeqMeta& meta, const ChunkSplits& splits, int wgs) {
