@@ -325,9 +325,10 @@ int cb_device_status(cb_ctx *ctx, int32_t *status);
  * ------------------------------------------------------------------------------------------------ */
 
 /* Options; unknown names give CB_EINVAL.
- *   "splits"     force the number of KV-sequence splits (0 = automatic)
+ *   "splits"     force the number of KV-sequence splits (0 = automatic); of cb_chunk_attention_device's longest sequence, as far as
+ *                the workspace goes
  *   "attn_impl"  0 or 2 = the matrix-core kernel of the configuration's type, 1 = scalar kernel (at most 8
- *                splits in bf16; for comparisons)
+ *                splits in bf16; for comparisons); cb_chunk_attention_device's takes a row at a time
  *   "stages"     bit mask of the steps cb_verify_tree_device enqueues (1 ancestor sets, 2 attention,
  *                4 argmax, 8 acceptance; default 15) -- for timing one step in isolation; with a
  *                step left out the results of the call are those of an earlier call or undefined
@@ -341,7 +342,8 @@ int cb_device_status(cb_ctx *ctx, int32_t *status);
  *                    0 = automatic)
  *   "tile_rows"      query rows of a workgroup of the bf16 MFMA kernels: 64, 128 or 256 where a kv head has as many, in
  *                    one round of workgroups and the sums stay in the class that the tallest tiles give them; not with
- *                    "splits" (0 = automatic)
+ *                    "splits" (0 = automatic).  For cb_chunk_attention_device any size, with "splits" or without, heads of 64
+ *                    at most 128
  *   "coop_merge"     0 = never merge the splits cooperatively (default 1: a grid that fits the
  *                    machine in one round has every workgroup of a tile merge a slice of it; otherwise,
  *                    and with 0, the last workgroup of a tile to finish merges it, or a merge kernel)

@@ -62,13 +62,13 @@ __device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16
   }
 }
 
-// The sweep of one workgroup whose tile has RW row groups of R row tiles each, up to its output rows (a single split) or its
-// partial state.  Without CARE it returns true where the tile has to be swept with.
-template <int D, bool PG, int R, int RW, bool CARE>
-__device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& jb, TileLds& sh, uint4* ring) {
+// Tiles of up to 64 rows, two row groups of a row tile each and two wavefronts to a group, which take the units in turn: the sweep of one workgroup
+// up to its output rows (a single split) or its partial state.  Without CARE it returns true where the tile has to be swept with.
+template <int D, bool PG, bool CARE>
+__device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb, TileLds& sh, uint4* ring) {
   using Part = PartialLayout<D, 32, true>;
   using F = Feed<D, kWideWaves, 32>;
-  constexpr int KW = kWideWaves / RW;    // key groups
+  constexpr int R = 1, RW = 2, KW = kWideWaves / RW;   // row tiles of a row group, row groups, key groups
   constexpr int NS = F::kSlots, PRO = F::kPrologue;
   // (scores run one stage ahead of the softmax: two stages are resident while a third is requested)
   static_assert(3 * KW <= NS && KW <= PRO, "a stage is requested in full while the one before it is worked on");
@@ -115,12 +115,7 @@ __device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& 
 #pragma unroll
   for (int t = 0; t < R; t++)
 #pragma unroll
-    for (int ds = 0; ds < D / 16; ds++) {
-      asm volatile("" : "+v"(st[t].q[ds]));  // (older than every unit)
-#ifdef __HIP_DEVICE_COMPILE__
-      if (R > 1) asm volatile("" : "+a"(st[t].q[ds]));  // (two tiles' queries live in accumulation registers)
-#endif
-    }
+    for (int ds = 0; ds < D / 16; ds++) asm volatile("" : "+v"(st[t].q[ds]));  // (older than every unit)
 
   // At the barrier in front of unit u NS - 2 units from u on have been requested.  It waits until those up to u + 3 have
   // landed; everybody is then done with those below u, whose places take the next requests.
@@ -168,8 +163,7 @@ __device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& 
     floatx16 sc[R];
     float mx[R];
     auto check = [&] {
-      bool raise = mx[0] > st[0].top;  // (false for NaN)
-      if (R > 1) raise |= mx[R - 1] > st[R - 1].top;
+      const bool raise = mx[0] > st[0].top;  // (false for NaN)
       if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {
 #pragma unroll
         for (int t = 0; t < R; t++) raise_reference<D>(st[t], mx[t], c2);
@@ -193,34 +187,29 @@ __device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& 
     check();
     int s = 0;
     // A step: the scores of stage s + 1 beside the exponentials of stage s, then its values; two at a time (the scores alternate between two
-    // sets of registers), the requests spread over the steps (all at once they hold up the wave that makes them).  With one key group
-    // a barrier for two steps.
-    auto step = [&](const floatx16 (&from)[R], floatx16 (&to)[R], bool barrier, bool masks) {  // from: the scores of stage s, to: those of stage s + 1
-      if (barrier) ready();
+    // sets of registers), the requests spread over the steps (all at once they hold up the wave that makes them).
+    auto step = [&](const floatx16 (&from)[R], floatx16 (&to)[R], bool masks) {  // from: the scores of stage s, to: those of stage s + 1
+      ready();
       if (masks) look(s);
       int64_t off[KW][F::kParts];
       uint32_t dst[KW];
 #pragma unroll
       for (int x = 0; x < KW; x++) feed.next(off[x], dst[x]);
-      if (KW > 1) read_k<D>(lane_k + at1, k);
+      read_k<D>(lane_k + at1, k);
       score_half<D, false, R, KW * F::kReq>(k, st, from, to, pw, lane_v + at, v, c2, [&](int i) {
         feed.request(i % F::kReq, off[i / F::kReq], dst[i / F::kReq]);
       });
       if (masks) mask(s + 1, to);
-      add_half<D, false, R, KW == 1>(k, lane_k + at2, lane_v + at, v, st, pw, to, mx, ones);
+      add_half<D, false, R, false>(k, lane_k + at2, lane_v + at, v, st, pw, to, mx, ones);
       if (masks) odd_max(s + 1);
       check();
       advance();
       s++;
     };
     first_ready();
-    if (nst > 1 && KW == 1) {  // (K operands are a step ahead in registers)
-      ready();
-      read_k<D>(lane_k + at1, k);
-    }
     while (s + 2 < nst && !masked(s + 2)) {
-      step(sc, sd, true, false);
-      step(sd, sc, KW > 1, false);
+      step(sc, sd, false);
+      step(sd, sc, false);
     }
     bf16x8 pb[R][2];
     auto add_unit = [&] {
@@ -240,8 +229,7 @@ __device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& 
     };
     // Stages with masks, one at a time.
     while (s + 1 < nst) {
-      const bool barrier = KW > 1 || (s & 1) == 0;
-      step(sc, sd, barrier, true);
+      step(sc, sd, true);
 #pragma unroll
       for (int t = 0; t < R; t++) sc[t] = sd[t];
     }
@@ -308,20 +296,13 @@ __device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& 
   else if (has_rows) sweep();
   else {  // no rows of its own: it only brings its share, passing the same barriers
     first_ready();
-    if (nst > 1 && KW == 1) ready();
     int s = 0;
-    auto step = [&](bool barrier) {
-      if (barrier) ready();
+    for (; s + 1 < nst; s++) {
+      ready();
       look(s);
       feed.request_units(KW);
       advance();
-      s++;
-    };
-    while (s + 2 < nst) {
-      step(true);
-      step(KW > 1);
     }
-    if (s + 1 < nst) step(true);
     look(s);
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
@@ -341,45 +322,34 @@ __device__ __forceinline__ bool sweep_chunk(const AttnParams& p, const TileJob& 
   };
   floatx4* const park = reinterpret_cast<floatx4*>(ring);
   float2* const park_ml = reinterpret_cast<float2*>(ring + kWideWaves * R * P * 64);
-  if constexpr (KW > 1) {
-    __syncthreads();  // every wave is done with the ring
-    static_assert(kWideWaves * R * (P * 64 + 32) <= F::kRingVecs, "");
+  __syncthreads();  // every wave is done with the ring
+  static_assert(kWideWaves * R * (P * 64 + 32) <= F::kRingVecs, "");
 #pragma unroll
-    for (int t = 0; t < R; t++) {
+  for (int t = 0; t < R; t++) {
 #pragma unroll
-      for (int pc = 0; pc < P; pc++) park[((w * R + t) * P + pc) * 64 + l] = piece(t, pc);  // (w = kw * RW + rw)
-      park_ml[(w * R + t) * 64 + l] = float2{st[t].mref, st[t].lacc[0]};
-    }
-    __syncthreads();
+    for (int pc = 0; pc < P; pc++) park[((w * R + t) * P + pc) * 64 + l] = piece(t, pc);  // (w = kw * RW + rw)
+    park_ml[(w * R + t) * 64 + l] = float2{st[t].mref, st[t].lacc[0]};
   }
+  __syncthreads();
 #pragma unroll
   for (int t = 0; t < R; t++) {
     floatx4 f[PP];
-    float lsum, mfin;
-    if constexpr (KW > 1) {
-      float2 ml[KW];
-      mfin = -INFINITY;
+    float2 ml[KW];
+    float lsum = 0.f, mfin = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < KW; k++) {
-        ml[k] = park_ml[((k * RW + rw) * R + t) * 64 + l];
-        mfin = fmaxf(mfin, ml[k].x);
-      }
-      const float mu = (mfin == -INFINITY) ? 0.f : mfin;
-      lsum = 0.f;
+    for (int k = 0; k < KW; k++) {
+      ml[k] = park_ml[((k * RW + rw) * R + t) * 64 + l];
+      mfin = fmaxf(mfin, ml[k].x);
+    }
+    const float mu = (mfin == -INFINITY) ? 0.f : mfin;
 #pragma unroll
-      for (int i = 0; i < PP; i++) f[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < PP; i++) f[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KW; k++) {
-        const float wt = __builtin_amdgcn_exp2f((ml[k].x - mu) * c2);
-        lsum += ml[k].y * wt;
+    for (int k = 0; k < KW; k++) {
+      const float wt = __builtin_amdgcn_exp2f((ml[k].x - mu) * c2);
+      lsum += ml[k].y * wt;
 #pragma unroll
-        for (int i = 0; i < PP; i++) f[i] += park[(((k * RW + rw) * R + t) * P + kw * PP + i) * 64 + l] * wt;
-      }
-    } else {
-      lsum = st[t].lacc[0];
-      mfin = st[t].mref;
-#pragma unroll
-      for (int i = 0; i < PP; i++) f[i] = piece(t, i);
+      for (int i = 0; i < PP; i++) f[i] += park[(((k * RW + rw) * R + t) * P + kw * PP + i) * 64 + l] * wt;
     }
     write_rows<D, 32, true, PP>(p, jb, rw * R + t, grow[t], f, kw * PP, mfin, lsum, c2, kw == 0, l);
   }
@@ -438,7 +408,7 @@ __device__ __forceinline__ void sweep_tall(const AttnParams& p, const TileJob& j
     for (int ds = 0; ds < D / 16; ds++) {
       asm volatile("" : "+v"(st[t].q[ds]));  // (older than every unit)
 #ifdef __HIP_DEVICE_COMPILE__
-      if (R > 1) asm volatile("" : "+a"(st[t].q[ds]));  // (two tiles' queries live in accumulation registers)
+      asm volatile("" : "+a"(st[t].q[ds]));  // (two tiles' queries live in accumulation registers)
 #endif
     }
 
@@ -959,7 +929,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_few(AttnParams p_a
   pin_args(p);
   TileJob jb;
   if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
-  if (sweep_chunk<D, PG, 1, 2, false>(p, jb, sh, ring)) sweep_chunk<D, PG, 1, 2, true>(p, jb, sh, ring);
+  if (sweep_few<D, PG, false>(p, jb, sh, ring)) sweep_few<D, PG, true>(p, jb, sh, ring);
   if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
 }
 

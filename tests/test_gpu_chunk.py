@@ -163,3 +163,60 @@ def test_long_caches_and_far_slots():
     size = np.einsum("qkh,khd->qhd", p, np.abs(to_np(new[2])).astype(np.float64)) / (s + p.sum(1))[:, :, None]
     # (the denominator's 600000 additions of ones in 32 bits, 16 keys to an accumulation: exact below 2^24)
     assert (np.abs(to_np(out) - want) <= 2 ** -5 * size + 1e-12).all()
+
+
+@pytest.mark.parametrize("dtype, hq, hkv, d", [("bf16", 8, 2, 128), ("bf16", 8, 4, 64), ("f32", 4, 2, 128)])
+@pytest.mark.parametrize("block", [1, 2, 16])
+@pytest.mark.parametrize("rows, splits", [(64, 1), (128, 2), (256, 1)])
+def test_long_block_tables(dtype, hq, hkv, d, block, rows, splits):
+    """More table entries than are kept at a time, and entries behind a sequence's last block that mean nothing."""
+    import torch
+    print(f"[case] tables {dtype} {hq}/{hkv} d{d} block {block} rows {rows} splits {splits}", flush=True)
+    b = Batch(dtype, hq, hkv, d, [5000, 17, 2900], [50, 1, 90], block, seed=block)
+    for i in range(3):
+        used = (int(b.kv_len[i]) + b.new[i] + block - 1) // block
+        b.table[i, used:] = torch.tensor([-7, 2**31 - 1, 2**20], dtype=torch.int32, device="cuda").repeat(b.table.shape[1])[:b.table.shape[1] - used]
+    b.ver.set_option("tile_rows", rows)
+    b.ver.set_option("splits", splits)
+    out = b.ver.chunk_attention(b.q, b.kv, b.kv_len, b.off)
+    torch.cuda.synchronize()
+    _check(b, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("max_splits", [1, 0])
+def test_a_small_workspace_takes_any_chunk(dtype, max_splits):
+    """max_nodes 1: chunks of any length all the same; 64 sequences, some with nothing new."""
+    import torch
+    lens, new = [(97 * i) % 600 for i in range(64)], [(0, 1, 1, 5, 70)[i % 5] for i in range(64)]
+    b = Batch(dtype, 8, 2, 64, lens, new, 16, seed=2, max_nodes=1, max_depth=1, max_splits=max_splits)
+    out = b.ver.chunk_attention(b.q, b.kv, b.kv_len, b.off)
+    torch.cuda.synchronize()
+    _check(b, out)
+
+
+def test_two_contexts_on_two_streams():
+    """Launches whose tiles' workgroups wait for each other, from two contexts at once."""
+    import torch
+    bs = [Batch("bf16", 32, 8, 128, [4000], [1], 16, seed=s, scale=2.0) for s in (1, 2)]
+    streams = [torch.cuda.Stream() for _ in bs]
+    outs = [torch.empty_like(b.q) for b in bs]
+    calls = [b.ver.bind_chunk_attention(b.q, b.kv, b.kv_len, b.off, o, stream=st) for b, o, st in zip(bs, outs, streams)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c in calls:
+            c()
+    torch.cuda.synchronize()
+    for b, o in zip(bs, outs):
+        _check(b, o)
+
+
+@pytest.mark.parametrize("splits", [1, 4])
+def test_heads_and_batches_that_fill_no_tile(splits):
+    """16 heads to a kv head, and a batch of 64 single tokens beside two longer chunks."""
+    import torch
+    b = Batch("bf16", 16, 1, 128, [300 + 41 * i for i in range(62)] + [0, 1000], [1] * 62 + [33, 20], 16, seed=4, scale=2.0)
+    b.ver.set_option("splits", splits)
+    out = b.ver.chunk_attention(b.q, b.kv, b.kv_len, b.off)
+    torch.cuda.synchronize()
+    _check(b, out)

@@ -169,3 +169,28 @@ def test_token_logprobs_checks_its_arguments(kw, code, text):
     rc, err = _check("logprobs", C.byref(cfg), p(a["logits"]), C.c_int64(a["stride"]), a["rows_of"], a["n"], p(a["rows"]), p(a["tokens"]), p(a["lp"]), p(a["ent"]), a["k"],
                      p(a["ids"]), p(a["tops"]))
     assert rc == code and text in err, (rc, err)
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_the_plan_covers_a_chunk(seed):
+    """Splits cover the longest sequence, jobs are counted as the kernel counts them, and options are kept to."""
+    rng = np.random.default_rng(seed)
+    g, hkv, d, dtype = int(rng.choice([1, 2, 4, 5, 16])), int(rng.choice([1, 2, 8])), int(rng.choice([64, 128])), str(rng.choice(["bf16", "f32"]))
+    batch, max_splits = int(rng.choice([1, 3, 64])), int(rng.choice([0, 1, 7]))
+    n = [int(rng.choice([0, 1, 1, 7, 64, 700, 5000])) for _ in range(batch)]
+    n[int(rng.integers(batch))] = 1 + int(rng.integers(300))
+    s = [int(rng.choice([0, 1, 100, 3000, 70000, 10**6])) for _ in range(batch)]
+    cfg = B.make_config(g * hkv, hkv, d, dtype, dtype, batch, int(rng.choice([1, 64])), 1, 100, 16, max_splits)
+    off = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    L, ip = B.load(), C.POINTER(C.c_int32)
+    for rows, splits in ((0, 0), (64, 0), (128, 5), (256, 1), (0, 64)):
+        plan = (C.c_int32 * 5)()
+        assert L.cb_debug_chunk_plan(C.byref(cfg), batch, np.array(s, dtype=np.int32).ctypes.data_as(ip), off.ctypes.data_as(ip), splits, rows, plan) == B.CB_OK
+        tile, ns, keys, jobs, tiles = plan
+        assert tile in ((16, 32) if dtype == "f32" else (64, 128, 256) if d == 128 else (64, 128))
+        if rows and dtype == "bf16":
+            assert tile == min(rows, 256 if d == 128 else 128)
+        assert tiles == max(-(-x * g // tile) for x in n)
+        assert 1 <= ns <= 1024 and (max_splits == 0 or ns <= max_splits) and (splits == 0 or ns <= splits)
+        if batch == 1:
+            assert keys % 32 == 0 and ns == -(-(s[0] + n[0]) // keys) and jobs == tiles * hkv * ns
