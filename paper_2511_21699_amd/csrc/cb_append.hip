@@ -3,6 +3,9 @@
 // A head x of D dims becomes y = x / sqrt(mean(x^2) + eps) * w, and then every pair (a, b) of its leading rotary dims
 // (a cos - b sin, b cos + a sin) of the token's position times the pair's frequency.  All of it in 32 bits, rounded once at the store;
 // the angle is reduced to a turn in 64 bits, because position * frequency in 32 bits is off by a thousandth of a radian at position 30000.
+//
+// What bounds it: memory, every head once in and once out: 8192 tokens of 32/32 heads of 128 in bf16, 403 MB, 74 us, 5.4 TB/s.  A few tokens take
+// what a launch takes, 3.5 to 5 us, the fifth of a microsecond for the angles and a tree's depths in it.
 #include "cb_internal.h"
 
 namespace cb {
@@ -44,7 +47,7 @@ struct Elems<__bf16> {
 
 constexpr int kAppendThreads = 256;
 
-// One workgroup per token.  A group of D / 2 / N lanes has a head: a lane holds two 16-byte pieces, dims N c .. and those half of the
+// One workgroup per token, so that a single token has its loads under way at once, all its heads', and its angles are worked out once.  A group of D / 2 / N lanes has a head: a lane holds two 16-byte pieces, dims N c .. and those half of the
 // rotated dims further (of the leading ones; of the others, pieces N c .. and half of those further), so that a rotation's pairs are a
 // lane's own.
 template <typename T, int D>

@@ -2,7 +2,9 @@
 //
 // Token i of a sequence with S cached slots attends to slots 0 .. S + i: o = sum_j p_j v_j / sum_j p_j, p_j = exp(scale q.k_j - m), in one
 // pass with the running maximum m; everything in 32 bits.  A wavefront takes 64 keys at a time: a lane scores one, then owns D / 64 dims
-// of the sum.
+// of the sum.  It takes every shape, at the pace of the plain arithmetic and with K and V read once per row: for blocks of a size that is no
+// power of two in bf16, whose keys the matrix-core kernels' loads could not place with shifts, and to compare with.  2048 tokens of 32/32
+// heads of 128 behind nothing take 3.0 ms, on the matrix cores 55 us.
 #include "cb_internal.h"
 
 namespace cb {

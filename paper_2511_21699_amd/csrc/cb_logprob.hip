@@ -6,12 +6,16 @@
 //
 // The likeliest tokens are ordered by one 64-bit word per entry that grows with the value and, among equal values, with falling index
 // (amax_word).  A wavefront's bound is the k-th largest of its lanes' maxima, which at least k entries reach and hardly more do
-// (of 4096 normal ones 24 reach the 20th, 44 the 32nd); those that reach it go to a list in LDS, which is cut to its k
-// largest at the end.  Of entries equal to the bound the first k (rounded up to a stretch of 64 pieces) are enough: so a row of
+// (of 4096 normal ones 24 reach the 20th, 44 the 32nd).  16-byte pieces whose largest entry reaches the bound of that moment wait in LDS; when they
+// are many, and at the end with the last bound, which is higher, their entries that reach it go to a list, which is cut to its k
+// largest.  Of entries equal to the bound the first k (rounded up to a stretch of 64 pieces) are enough: so a row of
 // equal entries, or one with few allowed tokens, does not fill the list.
 //
 // A workgroup takes a row, or a part of one where there are few rows; parts meet through the workspace, and the last to arrive puts them
 // together.
+//
+// What bounds it: many rows memory (2048 of 33333 in fp32, 273 MB, 54 us, 5.0 TB/s), beside two exponentials' worth of arithmetic per entry; few rows
+// what follows the sweep, a launch and, with parts, two round trips to memory (one row of 32000 in bf16 8.4 us, 40 of 128256 with the 20 largest 14.7).
 #include <float.h>
 
 #include <algorithm>
@@ -418,13 +422,14 @@ hipError_t launch_waves(hipStream_t st, const LogprobArgs& a) {
 // two blocks, so rows that fill the chip are taken by few wavefronts, and where they do not, a wavefront has a block or two.  In us, with
 // 1, 2, 4 and 8 wavefronts: 4096 rows of 1000 bf16 9.7, 14.7, 21.8, 45.5; 2048 of 32000 44.0, 39.8, 44.0, 50.4; 545 of 128256 108.9, 75.8, 53.4, 60.2;
 // 256 of 128256 106.4, 65.6, 40.7, 34.9.  One row of 32000 in 2 parts 9.6, in 4 8.3; one of 128256 in 8 12.2, in 16 16.3.
+// In parts, with 4 and 8 wavefronts: 16 rows of 128256 in 8 14.0, 18.6; 60 in 4 18.1, 17.4; 100 in 2 25.3, 20.9; 14 rows of 5000 (one part; with 2 8.3) 7.5, 7.6.
 hipError_t launch_logprob(hipStream_t st, const LogprobArgs& args) {
   LogprobArgs a = args;
   const int64_t blocks = ((int64_t)a.V * (a.is_f32 ? 4 : 2) + kLpBlock * 16 - 1) / (kLpBlock * 16);
   a.parts = a.n > kLpWgs / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({kLpParts, kLpWgs / a.n, blocks / 4}));
   if (blocks <= 2) return launch_waves<1>(st, a);
-  if (a.n >= 1024 || blocks <= 4) return launch_waves<2>(st, a);
-  if (a.n >= 384 || a.parts > 1) return launch_waves<4>(st, a);
+  if (a.n >= 1024 || (blocks <= 4 && a.n >= 384)) return launch_waves<2>(st, a);
+  if (a.n >= 384 || blocks <= 4 || (a.parts > 2 && blocks < 12 * a.parts)) return launch_waves<4>(st, a);
   return launch_waves<8>(st, a);
 }
 
