@@ -1270,6 +1270,8 @@ int check_chunk(cb_ctx* ctx, int32_t batch, const void* q, const cb_kv_layer* kv
   a.total = rc ? 0 : token_offsets[batch];
   if (a.total == 0) return rc;  // (nothing new: there need not be tensors)
   if (!q || !attn_out) return set_err(ctx, CB_EINVAL, "null argument");
+  for (int b = 0; b < batch; b++)  // (a kv head's rows are counted in 32 bits)
+    if ((int64_t)(token_offsets[b + 1] - token_offsets[b]) * (c.num_q_heads / c.num_kv_heads) > (1ll << 30)) return set_err(ctx, CB_EINVAL, "sequence %d has too many tokens", b);
   if (((uintptr_t)q | (uintptr_t)attn_out) & 15) return set_err(ctx, CB_EINVAL, "device pointers must be 16-byte aligned");
   a.q = q;
   a.out = attn_out;

@@ -140,6 +140,13 @@ def test_chunk_attention_checks_its_arguments(kw, code, text):
     assert rc == code and text in err, (rc, err)
 
 
+def test_chunk_attention_counts_rows_in_32_bits():
+    cfg, kv = B.make_config(**CFG), B.CbKvLayer(4 * A, 5 * A, 1 << 30, None, 0, 0)
+    for n, code in ((1 << 28, B.CB_OK), ((1 << 28) + 1, B.CB_EINVAL)):  # four heads to a kv head
+        rc, err = _check("chunk", C.byref(cfg), 1, C.c_void_p(1 << 60), C.byref(kv), _ints(5), _ints(0, n), C.c_void_p(1 << 61))
+        assert rc == code and (rc == B.CB_OK or "too many tokens" in err)
+
+
 @pytest.mark.parametrize("kw, code, text", [
     (dict(), B.CB_OK, ""),
     (dict(logits=A + 2), B.CB_OK, ""),
