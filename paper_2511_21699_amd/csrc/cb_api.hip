@@ -1091,8 +1091,8 @@ struct ChunkPlan {
   ChunkSplits splits;
 };
 
-// The cheapest of a few plans by an estimate of the launch's time, in us.  A sequence is cut into as many equal splits as its length has of the
-// longest's, so that jobs are of about one length.  A job takes `start` beside its sweep and `alone` for every 32 keys where it has a compute
+// The cheapest of a few plans by an estimate of the launch's time, in us.  A tile is cut into as few equal splits as keep to one length for the
+// whole batch, so that jobs are of about one length.  A job takes `start` beside its sweep and `alone` for every 32 keys where it has a compute
 // unit for itself; a compute unit gets through 32 keys of a tile in `full`, with as many workgroups as it holds, at the clock of a busy chip.  The longest
 // are dispatched first (chunk_job), so a launch ends with its longest job or, where there are more jobs than places, when the work is shared out
 // and what is left of a round of the shortest is through.  Reading the cache takes its time beside that, and both slow each other down where they are
@@ -1122,8 +1122,8 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     double dim64;                            // alone and full at head_dim 64
   };
   // From launches of 1 to 8192 tokens of 32/8 and 32/32 heads over up to 65536 keys.  With tiles of 64, 128 and 256 rows 8192 tokens from the first take
-  // 730, 533 and 543 us, 4096 behind 28672 3089, 2102 and 1901, 256 behind 30000 in one split 387, 569 and 777, in eight 240, 156 and 131.
-  static const Tile kBf16[] = {{64, 0.36, 0.36, 6.0, 2.0, 2.5, 0.78}, {128, 0.66, 0.52, 4.5, 2.5, 5.0, 0.7}, {256, 0.86, 0.96, 8.0, 4.0, 10.0, 1.0}};
+  // 726, 533 and 516 us, 4096 behind 28672 3059, 2102 and 1821, 256 behind 30000 in one split 382, 569 and 792, in eight 240, 156 and 131.
+  static const Tile kBf16[] = {{64, 0.36, 0.36, 5.5, 2.0, 2.5, 0.78}, {128, 0.66, 0.52, 4.5, 3.2, 5.0, 0.7}, {256, 0.86, 0.96, 8.0, 4.0, 10.0, 1.0}};
   static const Tile kF32[] = {{16, 0.75, 0.75, 6.0, 1.0, 6.0, 0.6}, {32, 1.4, 1.4, 8.0, 1.0, 6.0, 0.6}};
   ChunkPlan best{};
   double best_us = 0;
@@ -1141,19 +1141,22 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     int most = 1;
     if (tiles > 0 && tiles <= 1024 && (int64_t)batch * Hkv * tiles_max <= tickets)
       most = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(lay.total - lay.partial) / per_split, most_here, lay.max_splits, (len_max + 63) / 64, 4096 / tiles}));
-    int ns = opt_splits > 0 ? std::min(opt_splits, most) : 1;
-    for (int last = 0;; ns += 1 + ns / 12) {
-      ns = std::min(ns, most);
-      if (ns == last) break;
-      last = ns;
-      const int target = (len_max + ns - 1) / ns;
+    // Splits of the longest sequence, in tenths: 1.2 and 1.5 cut only the longest of tiles that differ in length (a prompt of 2048, 32/32 heads, in one
+    // split 55.8 us, in 1.2 53.8, in two 60; of 1024 28.1, 24.2 and 26.5).
+    auto next = [](int t) { return t < 12 ? 12 : t < 15 ? 15 : t < 20 ? 20 : t + 10 + t / 120 * 10; };
+    int tenths = opt_splits > 0 ? 10 * std::min(opt_splits, most) : 10;
+    for (int last = 0;; tenths = next(tenths)) {
+      tenths = std::min(tenths, 10 * most);
+      if (tenths == last) break;
+      last = tenths;
+      const int target = (int)((10ll * len_max + tenths - 1) / tenths);
       ChunkPlan p{rows, 1, 0, tiles_max, {}};
-      double work = 0, longest = 0, shortest = 1e30;  // in units of 32 keys
+      double work = 0, longest = 0, cut = 0, shortest = 1e30;  // in units of 32 keys; cut: the longest of a tile that is merged
       int64_t real = 0, merged = 0;
       for (int b = 0; b < batch; b++) {
         const int n = off[b + 1] - off[b], s = kv_len[b], len = s + n, nt = (int)(((int64_t)n * g + rows - 1) / rows);
         if (n == 0) continue;
-        const int parts = (len + target - 1) / target, chunk = ((len + parts - 1) / parts + 31) / 32 * 32, ns_b = (len + chunk - 1) / chunk;
+        const int chunk = (std::min(len, target) + 31) / 32 * 32, ns_b = (len + chunk - 1) / chunk;
         p.splits.keys[b] = chunk;
         p.nsplit = std::max(p.nsplit, ns_b);
         p.jobs += (int64_t)nt * Hkv * ns_b;
@@ -1165,19 +1168,20 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
           real += (int64_t)nt * Hkv;
           continue;
         }
-        for (int t = 0; t < nt; t++) {
-          const int tl = s + (int)((std::min<int64_t>((int64_t)(t + 1) * rows, (int64_t)n * g) - 1) / g) + 1, whole = tl / chunk, rest = tl - whole * chunk;
-          work += (whole * (chunk / 32) + (rest + 31) / 32) * (double)Hkv;
-          longest = std::max(longest, (double)(whole ? chunk / 32 : (rest + 31) / 32));
-          shortest = std::min(shortest, (double)(rest ? (rest + 31) / 32 : chunk / 32));
-          real += (int64_t)(whole + (rest > 0)) * Hkv;
-          merged += whole + (rest > 0) > 1 ? Hkv : 0;
+        for (int t = 0; t < nt; t++) {  // (chunk_job's splits)
+          const int tl = s + (int)((std::min<int64_t>((int64_t)(t + 1) * rows, (int64_t)n * g) - 1) / g) + 1, ns_t = (tl + chunk - 1) / chunk;
+          const int part = ((tl + ns_t - 1) / ns_t + 31) / 32, last = (tl + 31) / 32 - (ns_t - 1) * part;
+          work += (tl + 31) / 32 * (double)Hkv;
+          (ns_t > 1 ? cut : longest) = std::max(ns_t > 1 ? cut : longest, (double)part);
+          shortest = std::min(shortest, (double)last);
+          real += (int64_t)ns_t * Hkv;
+          merged += ns_t > 1 ? Hkv : 0;
         }
       }
       const double merge = p.nsplit == 1 ? 0.0 : p.jobs <= 256 ? tile.coop : tile.merge * std::min(p.nsplit + 1, 8);
-      const double places = two ? 512.0 : 256.0, one = longest * alone + start * (p.jobs > places ? 2 : 1) + merge, rounds = std::ceil(real / places) - real / places;
-      double shared = (work * full + real * (two ? 0.3 : 1.0) * start + merged * merge) / 256 + rounds * shortest * full;
-      if (two && real <= 512) shared = std::max((work * full + merged * merge) / 256, (longest + shortest) * full);
+      const double places = two ? 512.0 : 256.0, one = std::max(longest * alone, cut > 0 ? cut * alone + merge : 0.0) + start, rounds = std::ceil(real / places) - real / places;
+      double shared = (work * full + real * (two ? 0.2 : 1.25) * start + 0.5 * merged * merge) / 256 + rounds * shortest * full;
+      if (two && real <= 512) shared = std::max((work * full + 0.5 * merged * merge) / 256, (std::max(longest, cut) + shortest) * full);
       if (two) shared += start;
       const double sweep = real <= 256 ? one : std::max(one, shared), s2 = sweep * sweep, m2 = memory * memory;
       const double us = real > 256 && !two ? std::sqrt(s2 + m2) : std::sqrt(std::sqrt(s2 * s2 + m2 * m2));

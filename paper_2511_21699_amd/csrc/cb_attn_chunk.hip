@@ -8,9 +8,9 @@
 // statistics and partial states are in 32 bits.
 //
 // What bounds it, at 32/8 heads of 128: long sweeps the matrix cores beside the vector units, together all of a compute unit's time, at the 1.8 GHz that
-// this power allows (4096 tokens behind 28672 1.87 ms, 1100 TFLOP/s; the products alone 1250); single tokens reading the cache (16
+// this power allows (4096 tokens behind 28672 1.85 ms, 1110 TFLOP/s; the products alone 1250); single tokens reading the cache (16
 // sequences of up to 16384 105 us, 5.0 TB/s); short chunks a launch, a workgroup's start and the way of a split's state through memory (1024 tokens from
-// the first 23.5 us).  Hence three tiles, for a rule by the host: of 64 rows, whose workgroup has the whole ring of LDS for keys on their way, of
+// the first 24 us).  Hence three tiles, for a rule by the host: of 64 rows, whose workgroup has the whole ring of LDS for keys on their way, of
 // 128, two to a compute unit, and of 256, which read an operand from LDS for 64 rows.
 #include "cb_attn_wide.h"
 #include "cb_chunk.h"

@@ -4,13 +4,14 @@
 
 namespace cb {
 
-// The workgroup's (tile, split); lane_chunk: lane b has sequence b's keys per split.  p.grid_x: workgroups.  They are numbered sequence by sequence, the longest first, a sequence's tiles from the last, whose
-// sweep is the longest, to the first, then splits, and the kv head runs fastest: what is dispatched last is short, and with a
+// The workgroup's (tile, split); lane_chunk: lane b has the most keys of a split of sequence b.  p.grid_x: workgroups.  They are numbered sequence by sequence, the longest
+// first, a sequence's tiles from the last, whose sweep is the longest, to the first, then splits, and the kv head runs fastest: what is dispatched last is short, and with a
 // multiple of 8 kv heads a head's tiles share an XCD's L2.
 __device__ __forceinline__ bool chunk_job(const AttnParams& p, const SeqMetaLanes& ml, int lane_chunk, int d, TileJob& j) {
-  // Two workgroups to a compute unit: numbers 256 to 511 go where 0 to 255 have gone, in that order, so they are taken from the shortest on, in
+  // Two workgroups to a compute unit (tiles of 128 rows): numbers 256 to 511 go where 0 to 255 have gone, in that order, so they are taken from the shortest on, in
   // stretches of 8 that keep their XCD (a prompt of 2048, 32 heads: 64 stages and 1 on a compute unit instead of 64 and 32).
-  if (d >= 256 && d < 512 && p.grid_x % 8 == 0) {
+  // Where a compute unit has one workgroup at a time the next one dispatched is to be the longest left (fp32, 512 tokens, 32/8 heads: 45 us, and 53 that way).
+  if (p.tile_rows == 128 && d >= 256 && d < 512 && p.grid_x % 8 == 0) {
     const int end = p.grid_x < 512 ? p.grid_x : 512;
     d = 256 + end - 8 - (d & ~7) + (d & 7);
   }
@@ -31,10 +32,11 @@ __device__ __forceinline__ bool chunk_job(const AttnParams& p, const SeqMetaLane
   j.layer = 0;
   j.row0 = j.rt * p.tile_rows;
   const int last = (j.row0 + p.tile_rows < j.M ? j.row0 + p.tile_rows : j.M) - 1, len = s.S + last / j.g + 1;
-  j.k0 = j.split * chunk;
-  if (j.k0 >= len) return false;
-  j.k1 = j.k0 + chunk < len ? j.k0 + chunk : len;
   j.nsplit = (len + chunk - 1) / chunk;
+  if (j.split >= j.nsplit) return false;
+  const int part = ((len + j.nsplit - 1) / j.nsplit + 31) & ~31;  // (at most `chunk`: the tile's splits are of one length too)
+  j.k0 = j.split * part;
+  j.k1 = j.k0 + part < len ? j.k0 + part : len;
   return true;
 }
 
