@@ -1123,7 +1123,7 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
   };
   // From launches of 1 to 8192 tokens of 32/8 and 32/32 heads over up to 65536 keys.  With tiles of 64, 128 and 256 rows 8192 tokens from the first take
   // 726, 533 and 516 us, 4096 behind 28672 3059, 2102 and 1821, 256 behind 30000 in one split 382, 569 and 792, in eight 240, 156 and 131.
-  static const Tile kBf16[] = {{64, 0.36, 0.36, 5.5, 2.0, 2.5, 0.78}, {128, 0.66, 0.52, 4.5, 3.2, 5.0, 0.7}, {256, 0.86, 0.96, 8.0, 4.0, 10.0, 1.0}};
+  static const Tile kBf16[] = {{64, 0.36, 0.36, 5.5, 2.0, 4.0, 0.78}, {128, 0.66, 0.52, 4.5, 3.2, 5.0, 0.7}, {256, 0.86, 0.96, 8.0, 4.0, 10.0, 1.0}};
   static const Tile kF32[] = {{16, 0.75, 0.75, 6.0, 1.0, 6.0, 0.6}, {32, 1.4, 1.4, 8.0, 1.0, 6.0, 0.6}};
   ChunkPlan best{};
   double best_us = 0;
