@@ -1097,7 +1097,7 @@ struct ChunkPlan {
 // are dispatched first (chunk_job), so a launch ends with its longest job or, where there are more jobs than places, when the work is shared out
 // and what is left of a round of the shortest is through.  Reading the cache takes its time beside that, and both slow each other down where they are
 // about as long: more where one workgroup after the other has a compute unit, as then the long jobs of matrix products come first and the short ones
-// of single tokens, which read, last.  Splits have the room that the workspace has, and are not looked at past a few thousand jobs.
+// of single tokens, which read, last.  Splits have the room that the workspace has.
 ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, int opt_tile_rows, int batch, const int32_t* kv_len, const int32_t* off) {
   const bool f32 = c.qkv_dtype == CB_F32;
   const int g = c.num_q_heads / c.num_kv_heads, Hkv = c.num_kv_heads;
@@ -1140,7 +1140,7 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     for (int b = 0; b < batch; b++) tiles += ((int64_t)(off[b + 1] - off[b]) * g + rows - 1) / rows * Hkv;
     int most = 1;
     if (tiles > 0 && tiles <= 1024 && (int64_t)batch * Hkv * tiles_max <= tickets)
-      most = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(lay.total - lay.partial) / per_split, most_here, lay.max_splits, (len_max + 63) / 64, 4096 / tiles}));
+      most = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(lay.total - lay.partial) / per_split, most_here, lay.max_splits, (len_max + 63) / 64, 1024}));
     // Splits of the longest sequence, in tenths: 1.2 and 1.5 cut only the longest of tiles that differ in length (a prompt of 2048, 32/32 heads, in one
     // split 55.8 us, in 1.2 53.8, in two 60; of 1024 28.1, 24.2 and 26.5).
     auto next = [](int t) { return t < 12 ? 12 : t < 15 ? 15 : t < 20 ? 20 : t + 10 + t / 120 * 10; };
@@ -1189,7 +1189,7 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
         best = p;
         best_us = us;
       }
-      if (opt_splits > 0) break;
+      if (opt_splits > 0 || p.jobs > 1024) break;  // (more splits of what fills the chip several times gain nothing)
     }
   }
   return best;
