@@ -25,9 +25,10 @@ __device__ __forceinline__ void mask_chunk(floatx16& s, int key0, int seen, int 
 }
 
 // A value that a query must not see reaches its sum with weight 0, which hides it only if it is finite; and the denominator's MFMA has the
-// probabilities of two queries in a column, one of them times 0.  So where some query does not see a unit whole, infinities and NaN
-// among its values, and queries whose largest score is one, are looked out for, and a tile that has any is swept again with care: with 0 in
-// the place of infinities and NaN, and these added up separately for the queries that do see them.
+// probabilities of two queries in a column, one of them times 0, so that a query whose scores are not finite reaches another one's sum, wherever
+// the keys are.  So infinities and NaN are looked out for among the values of units that some query does not see whole, and among the denominators at
+// the end (what is no number stays none in a sum), and a tile that has any is swept again with care: with 0 in the place of infinities and NaN, and
+// values of these added up separately for the queries that do see them.
 __device__ __forceinline__ uint32_t odd_bits(const uintx4& x, uint32_t bits) {  // (an exponent of ones overflows into the sign's place: bits 15 and 31)
 #pragma unroll
   for (int i = 0; i < 4; i++) bits |= (x[i] & 0x7f807f80u) + 0x00800080u;
@@ -68,10 +69,24 @@ __device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16
   }
 }
 
+// Whether some wavefront of the workgroup met infinities or NaN; `odd`: the lane's bits (odd_bits), its denominators are looked at here.  A barrier.
+template <int D, int R>
+__device__ __forceinline__ bool any_odd(const TileState<D> (&st)[R], uint32_t odd, int (&seen)[kWideWaves], int w, int l) {
+#pragma unroll
+  for (int t = 0; t < R; t++) odd |= fabsf(st[t].lacc[0]) < INFINITY ? 0u : 0x8000u;
+  const bool mine = __builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0) != 0;
+  if (l == 0) seen[w] = mine;
+  __syncthreads();
+  int any = 0;
+#pragma unroll
+  for (int x = 0; x < kWideWaves; x++) any |= seen[x];
+  return any != 0;
+}
+
 // Tiles of up to 64 rows, two row groups of a row tile each and two wavefronts to a group, which take the units in turn: the sweep of one workgroup
 // up to its output rows (a single split) or its partial state.  Without CARE it returns true where the tile has to be swept with.
 template <int D, bool PG, bool CARE>
-__device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb, TileLds& sh, uint4* ring) {
+__device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb, TileLds& sh, int (&odd_waves)[kWideWaves], uint4* ring) {
   using Part = PartialLayout<D, 32, true>;
   using F = Feed<D, kWideWaves, 32>;
   constexpr int R = 1, RW = 2, KW = kWideWaves / RW;   // row tiles of a row group, row groups, key groups
@@ -184,12 +199,6 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
     mask(0, sc);
 #pragma unroll
     for (int t = 0; t < R; t++) mx[t] = row_max(sc[t]);
-    auto odd_max = [&](int s) {
-      if (!hides || !masked(s)) return;
-#pragma unroll
-      for (int t = 0; t < R; t++) odd |= mx[t] < INFINITY ? 0u : 0x8000u;
-    };
-    odd_max(0);
     check();
     int s = 0;
     // A step: the scores of stage s + 1 beside the exponentials of stage s, then its values; two at a time (the scores alternate between two
@@ -207,7 +216,6 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
       });
       if (masks) mask(s + 1, to);
       add_half<D, false, R, false>(k, lane_k + at2, lane_v + at, v, st, pw, to, mx, ones);
-      if (masks) odd_max(s + 1);
       check();
       advance();
       s++;
@@ -312,13 +320,8 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
     look(s);
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
-  if (!CARE && hides) {
-    if (tid == 0) sh.flag = 0;
-    __syncthreads();
-    if (__builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0) != 0 && l == 0) sh.flag = 1;
-    __syncthreads();
-    if (sh.flag) return true;
-  }
+  if (CARE) __syncthreads();  // every wave is done with the ring
+  else if (any_odd<D>(st, odd, odd_waves, w, l)) return true;
   // With two key groups each finishes one half of the pieces: all park their accumulators and (mref, l) in the
   // ring, then each adds up the groups' for its own pieces.
   constexpr int P = Part::P, PP = P / KW;
@@ -328,7 +331,6 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
   };
   floatx4* const park = reinterpret_cast<floatx4*>(ring);
   float2* const park_ml = reinterpret_cast<float2*>(ring + kWideWaves * R * P * 64);
-  __syncthreads();  // every wave is done with the ring
   static_assert(kWideWaves * R * (P * 64 + 32) <= F::kRingVecs, "");
 #pragma unroll
   for (int t = 0; t < R; t++) {
@@ -363,9 +365,10 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
 }
 
 // Tiles of up to 256 rows in long sweeps, four wavefronts of two row tiles, one workgroup to a compute unit: an operand read from LDS serves 64
-// rows.  Units that some query does not see whole, few there, are taken one at a time and with care in any case.
-template <int D, bool PG>
-__device__ __forceinline__ void sweep_tall(const AttnParams& p, const TileJob& jb, TileLds& sh, uint4* ring) {
+// rows.  Units that some query does not see whole, few there, are taken one at a time and with care in any case.  Without CARE it returns
+// true where all units have to be.
+template <int D, bool PG, bool CARE>
+__device__ __forceinline__ bool sweep_tall(const AttnParams& p, const TileJob& jb, TileLds& sh, int (&odd_waves)[kWideWaves], uint4* ring) {
   constexpr int R = 2;
   using Part = PartialLayout<D, 32, true>;
   using F = Feed<D, kWideWaves, 32>;
@@ -437,6 +440,7 @@ __device__ __forceinline__ void sweep_tall(const AttnParams& p, const TileJob& j
   };
   // this wave's stages whose units are all prefix and all inside the split (rounds down; may be negative: none)
   auto fast_stages = [&] {
+    if (CARE) return 0;
     const int n = ((S < k1 ? S : k1) - k0) / kUnitKeys;
     return nst < n ? nst : n;
   };
@@ -464,7 +468,7 @@ __device__ __forceinline__ void sweep_tall(const AttnParams& p, const TileJob& j
   };
   auto add_unit = [&](int s, const bf16x8 (&pb)[R][2], uint32_t place) {
     const uint32_t va = lane_v + place;
-    const bool careful = k0 + s * kUnitKeys + kUnitKeys > S;  // (uniform)
+    const bool careful = CARE || k0 + s * kUnitKeys + kUnitKeys > S;  // (uniform)
     bool odd = false, odd_p = false;
     // (the denominator's MFMA has the probabilities of two queries in a column, one of them times 0)
 #pragma unroll
@@ -565,6 +569,7 @@ __device__ __forceinline__ void sweep_tall(const AttnParams& p, const TileJob& j
     for (; s + 1 < nst; s++) top();
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
+  if (!CARE && any_odd<D>(st, 0, odd_waves, w, l)) return true;
 #pragma unroll
   for (int t = 0; t < R; t++) {
     floatx4 f[Part::P];
@@ -575,6 +580,7 @@ __device__ __forceinline__ void sweep_tall(const AttnParams& p, const TileJob& j
     }
     write_rows<D, 32, true, Part::P>(p, jb, w * R + t, grow[t], f, 0, st[t].mref, st[t].lacc[0], c2, true, l);
   }
+  return false;
 }
 
 // Tiles of up to 128 rows, four wavefronts of 32 rows, two workgroups to a compute unit: the one's start, tail and barriers are behind
@@ -587,6 +593,7 @@ struct ManyLds {
   uint4 ring[(kK + kV) * kBytes / 16];
   int bt[kBtLds];
   int flag;
+  int odd[kWideWaves];
 };
 
 // The memory side: K of a unit is requested two steps before its V, whose addresses wait in registers until then.
@@ -761,17 +768,11 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
     uint4 k[D / 16];
     uintx4 pw[R][2];
     bf16x8 v[D / 32];
-    auto odd_max = [&](int s) {
-      if (!hides || !masked(s)) return;
-#pragma unroll
-      for (int t = 0; t < R; t++) odd |= mx[t] < INFINITY ? 0u : 0x8000u;
-    };
     read_k<D>(lane_k, k);
     scores<D, R>(k, st, sc);
     mask(0, sc);
 #pragma unroll
     for (int t = 0; t < R; t++) mx[t] = row_max(sc[t]);
-    odd_max(0);
     check(mx);
     advance_k();
     read_k<D>(lane_k + k_at, k);
@@ -785,7 +786,6 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
       feed.requested(true, true);
       if (masks) mask(s + 1, to);
       add_half<D, false, R, true>(k, lane_k + k_at, lane_v + v_at, v, st, pw, to, mx, ones);
-      if (masks) odd_max(s + 1);
       check(mx);
       advance_k();
       advance_v();
@@ -870,13 +870,7 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
     look(nst - 1);
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
-  if (!CARE && hides) {
-    if (tid == 0) sh.flag = 0;
-    __syncthreads();
-    if (__builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0) != 0 && l == 0) sh.flag = 1;
-    __syncthreads();
-    if (sh.flag) return true;
-  }
+  if (!CARE && any_odd<D>(st, odd, sh.odd, w, l)) return true;
 #pragma unroll
   for (int t = 0; t < R; t++) {
     floatx4 f[Part::P];
@@ -931,11 +925,12 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_few(AttnParams p_a
   const int lane_chunk = splits.keys[threadIdx.x & 63];
   __shared__ __align__(1024) uint4 ring[Feed<D, kWideWaves, 32>::kRingVecs];
   __shared__ TileLds sh;
+  __shared__ int odd[kWideWaves];
   AttnParams p = p_arg;
   pin_args(p);
   TileJob jb;
   if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
-  if (sweep_few<D, PG, false>(p, jb, sh, ring)) sweep_few<D, PG, true>(p, jb, sh, ring);
+  if (sweep_few<D, PG, false>(p, jb, sh, odd, ring)) sweep_few<D, PG, true>(p, jb, sh, odd, ring);
   if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
 }
 
@@ -945,11 +940,12 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_tall(AttnParams p_
   const int lane_chunk = splits.keys[threadIdx.x & 63];
   __shared__ __align__(1024) uint4 ring[Feed<D, kWideWaves, 32>::kRingVecs];
   __shared__ TileLds sh;
+  __shared__ int odd[kWideWaves];
   AttnParams p = p_arg;
   pin_args(p);
   TileJob jb;
   if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
-  sweep_tall<D, PG>(p, jb, sh, ring);
+  if (sweep_tall<D, PG, false>(p, jb, sh, odd, ring)) sweep_tall<D, PG, true>(p, jb, sh, odd, ring);
   if (jb.nsplit == 1) return;
   if (p.coop_merge) split_merge<D, 32, true, kWideWaves, 256, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
   else merge_by_last<D>(p, jb, &sh.flag);

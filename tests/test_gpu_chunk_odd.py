@@ -1,0 +1,53 @@
+"""Attention of a chunk over the cache (cb_chunk_attention_device) where inputs are no numbers: who may see it, and who may not."""
+import pytest
+
+from .serving_gpu import Batch
+
+pytestmark = pytest.mark.gpu
+
+WHAT = [float("nan"), float("inf"), -float("inf")]
+
+
+def _options(b, rows=0, splits=0, coop=1):
+    for name, value in (("tile_rows", rows), ("splits", splits), ("coop_merge", coop)):
+        b.ver.set_option(name, value)
+
+
+def _attend(b):
+    import torch
+    out = b.ver.chunk_attention(b.q, b.kv, b.kv_len, b.off)
+    torch.cuda.synchronize()
+    return out
+
+
+def _spoil_queries(b, at):
+    """One head's query of one token: its own row is no number, and every other row is the same to the bit.  (An infinite entry gives scores of
+    both infinities over a few random keys, whose softmax is no number either.)"""
+    import torch
+    clean, kept = _attend(b), b.q.clone()
+    assert not clean.isnan().any()
+    for token, head in at:
+        for what in WHAT:
+            b.q[token, head, 3] = what
+            got = _attend(b)
+            b.q.copy_(kept)
+            assert got[token, head].isnan().all(), (token, head, what)
+            got[token, head] = clean[token, head]
+            assert torch.equal(got, clean), (token, head, what, (got != clean).any(-1).nonzero()[:4].tolist())
+
+
+@pytest.mark.parametrize("dtype, d, rows", [("bf16", 128, 64), ("bf16", 128, 128), ("bf16", 128, 256), ("bf16", 64, 64), ("bf16", 64, 128), ("f32", 128, 0)])
+@pytest.mark.parametrize("hq, hkv", [(2, 2), (8, 2), (16, 1)])
+@pytest.mark.parametrize("splits, coop", [(1, 1), (3, 1), (8, 1), (8, 0)])
+def test_a_query_that_is_no_number_spoils_its_own_row_alone(dtype, d, rows, hq, hkv, splits, coop):
+    print(f"[case] odd query {dtype} {d} {rows} {hq}/{hkv} {splits} {coop}", flush=True)
+    b = Batch(dtype, hq, hkv, d, [700, 90], [45, 1], 16, seed=splits, scale=2.0)
+    _options(b, rows, splits, coop)
+    _spoil_queries(b, [(44, hq - 1), (21, 0), (45, hq - 1)])
+
+
+@pytest.mark.parametrize("hq, hkv, d, kv_len, new, block", [(32, 8, 128, [4000], [3], 16), (32, 8, 128, [2500], [1], 0), (32, 32, 128, [0], [300], 0),
+                                                            (32, 8, 128, [9000], [256], 16), (32, 8, 64, [3000, 0], [100, 33], 16)])
+def test_odd_queries_with_the_plans_own_tiles(hq, hkv, d, kv_len, new, block):
+    b = Batch("bf16", hq, hkv, d, kv_len, new, block, seed=1, scale=2.0)
+    _spoil_queries(b, [(new[0] - 1, hq - 1), (new[0] // 2, hq // 2)])
