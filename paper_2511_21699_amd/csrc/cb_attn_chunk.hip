@@ -45,9 +45,10 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 a, bool& odd) {
   }
   return __builtin_bit_cast(bf16x8, x);
 }
-// p0, p1: the lane's probabilities (B operands); v_at: the unit's values in LDS.
+// p0, p1: the lane's probabilities (B operands); v_at: the unit's values in LDS; sees: how many of its keys the lane's query sees.  One whose probability is
+// 0 in 32 bits has a positive weight all the same, and an infinity or NaN times that is what it is.
 template <int D>
-__device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16x8& p0, const bf16x8& p1, uint32_t v_at, int l) {
+__device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16x8& p0, const bf16x8& p1, uint32_t v_at, int sees, int l) {
   const int r = l & 31, h = l >> 5;
   const uintx4 x0 = __builtin_bit_cast(uintx4, p0), x1 = __builtin_bit_cast(uintx4, p1);
   for (int kk = 0; kk < kUnitKeys; kk++) {
@@ -64,7 +65,7 @@ __device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16
       for (int v = 0; v < 16; v++) {
         const int dim = 32 * dt + 8 * (v >> 2) + 4 * h + (v & 3);
         const uint32_t x = *(const CB_LDS uint16_t*)(v_at + kk * (2 * D) + (((dim >> 3) ^ swizzle_v<D, 32>(kk)) << 4) + (dim & 7) * 2);
-        if ((x & 0x7f80u) == 0x7f80u && pk != 0.f) o[dt][v] += pk * __uint_as_float(x << 16);
+        if ((x & 0x7f80u) == 0x7f80u && kk < sees) o[dt][v] += (pk == 0.f ? 1.f : pk) * __uint_as_float(x << 16);
       }
   }
 }
@@ -302,7 +303,7 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
         }
       if (__builtin_amdgcn_ballot_w64(odd_v) != 0) {
 #pragma unroll
-        for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + at + kSlotBytes / 2, l);
+        for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + at + kSlotBytes / 2, (seen[t] < k1 ? seen[t] : k1) - k0 - (s * KW + kw) * kUnitKeys, l);
       }
     }
   };
@@ -487,7 +488,7 @@ __device__ __forceinline__ bool sweep_tall(const AttnParams& p, const TileJob& j
       }
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
 #pragma unroll
-      for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + place + kSlotBytes / 2, l);
+      for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + place + kSlotBytes / 2, (seen[t] < k1 ? seen[t] : k1) - k0 - s * kUnitKeys, l);
     }
   };
   auto sweep = [&] {
@@ -851,7 +852,7 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
           }
         if (__builtin_amdgcn_ballot_w64(odd_v) != 0)
 #pragma unroll
-          for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], vring + v_at, l);
+          for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], vring + v_at, (seen[t] < k1 ? seen[t] : k1) - k0 - s * kUnitKeys, l);
       }
       advance_k();
       advance_v();

@@ -199,7 +199,7 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_
         for (int e = 0; e < 4; e++)
 #pragma unroll
           for (int t = 0; t < RT; t++) o[t][n][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[x][n][e], pr[t][x], o[t][n][e], 0, 0, 0);
-    if (__builtin_expect(odd_v, 0)) {  // infinities or NaN among the unit's values, for the queries that do see them
+    if (__builtin_expect(odd_v, 0)) {  // infinities or NaN among the unit's values, for the queries that do see them, with a weight of 0 in 32 bits too
 #pragma unroll
       for (int x = 0; x < 4; x++)
         for (int part = 0; part < 4 && key0 + 4 * part + x < k1; part++) {
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(64 * kF32Waves, D == 64 && RT == 1 ? 4 : 2) void k_
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                   const float odd = vp[64 * n + 16 * h + 4 * i + e];
-                  o[t][n][e][i] += (is_finite(odd) || pk == 0.f) ? 0.f : pk * odd;
+                  o[t][n][e][i] += is_finite(odd) || key0 + 4 * part + x >= seen[t] ? 0.f : (pk == 0.f ? 1.f : pk) * odd;
                 }
           }
         }

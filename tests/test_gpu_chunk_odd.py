@@ -51,3 +51,33 @@ def test_a_query_that_is_no_number_spoils_its_own_row_alone(dtype, d, rows, hq, 
 def test_odd_queries_with_the_plans_own_tiles(hq, hkv, d, kv_len, new, block):
     b = Batch("bf16", hq, hkv, d, kv_len, new, block, seed=1, scale=2.0)
     _spoil_queries(b, [(new[0] - 1, hq - 1), (new[0] // 2, hq // 2)])
+
+
+TILES = [("bf16", 128, 64), ("bf16", 128, 128), ("bf16", 128, 256), ("bf16", 64, 64), ("bf16", 64, 128), ("f32", 128, 0), ("f32", 64, 0)]
+
+
+def _spoil_value(b, slot, seen_from, what):
+    """One entry of one value, of the sequence's kv head 1: rows from token seen_from on see it, whatever its weight; returns theirs."""
+    import torch
+    clean = _attend(b)
+    kept = b.v[0, slot, 1, 5].clone()
+    b.v[0, slot, 1, 5] = what
+    got = _attend(b)
+    b.v[0, slot, 1, 5] = kept
+    g = b.hq // b.hkv
+    rows = got[seen_from:b.new[0], g:2 * g, 5].clone()
+    got[seen_from:b.new[0], g:2 * g, 5] = clean[seen_from:b.new[0], g:2 * g, 5]
+    assert not clean.isnan().any() and torch.equal(got, clean)
+    return rows
+
+
+@pytest.mark.parametrize("dtype, d, rows", TILES)
+@pytest.mark.parametrize("splits", [1, 3])
+def test_values_come_through_whatever_their_weight(dtype, d, rows, splits):
+    """Scores hundreds apart: the weights of most values that a token sees are 0 in 32 bits, and in the formula they are not."""
+    print(f"[case] odd weightless value {dtype} {d} {rows} {splits}", flush=True)
+    b = Batch(dtype, 8, 2, d, [70], [60], seed=7, scale=100.0)
+    _options(b, rows, splits)
+    for what in WHAT:
+        for t in (0, 20, 59):
+            assert not _spoil_value(b, 70 + t, t, what).isfinite().any(), (what, t)
