@@ -24,17 +24,10 @@ __device__ __forceinline__ void mask_chunk(floatx16& s, int key0, int seen, int 
   for (int v = 0; v < 16; v++) s[v] = 8 * (v >> 2) + (v & 3) < n ? s[v] : -INFINITY;
 }
 
-// A value that a query must not see reaches its sum with weight 0, which hides it only if it is finite; and the denominator's MFMA has the
-// probabilities of two queries in a column, one of them times 0, so that a query whose scores are not finite reaches another one's sum, wherever
-// the keys are.  So infinities and NaN are looked out for among the values of units that some query does not see whole, and among the denominators at
-// the end (what is no number stays none in a sum), and a tile that has any is swept again with care: with 0 in the place of infinities and NaN, and
-// values of these added up separately for the queries that do see them.
-__device__ __forceinline__ uint32_t odd_bits(const uintx4& x, uint32_t bits) {  // (an exponent of ones overflows into the sign's place: bits 15 and 31)
-#pragma unroll
-  for (int i = 0; i < 4; i++) bits |= (x[i] & 0x7f807f80u) + 0x00800080u;
-  return bits;
-}
-
+// A value that a query must not see, or a split's last one in the places behind it, reaches a sum with weight 0, which hides it only if it is finite;
+// and the denominator's MFMA has the probabilities of two queries in a column, one of them times 0, so that a query whose scores are not finite
+// reaches another one's sum.  What is no number stays none in a sum, so every tile looks at its sums when its sweep is through, and one that has
+// infinities or NaN is swept again with care: with 0 in the place of those, and values of these added up separately for the queries that do see them.
 __device__ __forceinline__ bf16x8 finite_only(bf16x8 a, bool& odd) {
   uintx4 x = __builtin_bit_cast(uintx4, a);
 #pragma unroll
@@ -70,24 +63,31 @@ __device__ __forceinline__ void add_odd_values(floatx16 (&o)[D / 32], const bf16
   }
 }
 
-// Whether some wavefront of the workgroup met infinities or NaN; `odd`: the lane's bits (odd_bits), its denominators are looked at here.  A barrier.
+// Whether some wavefront's sums have infinities or NaN.  A barrier.
 template <int D, int R>
-__device__ __forceinline__ bool any_odd(const TileState<D> (&st)[R], uint32_t odd, int (&seen)[kWideWaves], int w, int l) {
+__device__ __forceinline__ bool any_odd(const TileState<D> (&st)[R], int (&odd)[kWideWaves], int w, int l) {
+  float x[4] = {};  // (times 0 and added up: 0 or NaN; four chains)
 #pragma unroll
-  for (int t = 0; t < R; t++) odd |= fabsf(st[t].lacc[0]) < INFINITY ? 0u : 0x8000u;
-  const bool mine = __builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0) != 0;
-  if (l == 0) seen[w] = mine;
+  for (int t = 0; t < R; t++) {
+    x[t] = fmaf(st[t].lacc[0], 0.f, x[t]);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; dt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) x[v & 3] = fmaf(st[t].o[dt][v], 0.f, x[v & 3]);
+  }
+  const bool mine = __builtin_amdgcn_ballot_w64((x[0] + x[1]) + (x[2] + x[3]) != 0.f) != 0;
+  if (l == 0) odd[w] = mine;
   __syncthreads();
   int any = 0;
 #pragma unroll
-  for (int x = 0; x < kWideWaves; x++) any |= seen[x];
+  for (int i = 0; i < kWideWaves; i++) any |= odd[i];
   return any != 0;
 }
 
 // Tiles of up to 64 rows, two row groups of a row tile each and two wavefronts to a group, which take the units in turn: the sweep of one workgroup
 // up to its output rows (a single split) or its partial state.  Without CARE it returns true where the tile has to be swept with.
 template <int D, bool PG, bool CARE>
-__device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb, TileLds& sh, int (&odd_waves)[kWideWaves], uint4* ring) {
+__device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb, TileLds& sh, int (&odd)[kWideWaves], uint4* ring) {
   using Part = PartialLayout<D, 32, true>;
   using F = Feed<D, kWideWaves, 32>;
   constexpr int R = 1, RW = 2, KW = kWideWaves / RW;   // row tiles of a row group, row groups, key groups
@@ -153,7 +153,6 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
   };
   // whether some query may not see some key of the stage, or the split ends in it (uniform in the workgroup)
   const int whole_end = S < k1 ? S : k1;
-  const bool hides = S < k1;  // (not for single tokens)
   auto masked = [&](int s) { return k0 + (s + 1) * KW * kUnitKeys > whole_end; };
   // Places in the ring, in bytes, of this wave's units of the current stage and the two behind it
   constexpr uint32_t kSlotBytes = F::kSlotBytes;
@@ -168,14 +167,6 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
   const uint32_t lane_v = (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + kSlotBytes / 2 + lane_v_byte<D>(l);
   const bf16x8 ones = half_ones(l);
 
-  uint32_t odd = 0;  // bits 15 and 31: infinities or NaN
-  auto look = [&](int s) {  // the stage's values, this wavefront's share
-    if (!hides || !masked(s)) return;
-    constexpr uint32_t kShare = kSlotBytes / 2 * KW / kWideWaves;
-    const uint32_t from = (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + at + kSlotBytes / 2 + rw * kShare + l * 16;
-#pragma unroll
-    for (uint32_t x = 0; x < kShare; x += 1024) odd = odd_bits(__builtin_bit_cast(uintx4, *(const CB_LDS uintx4*)(from + x)), odd);
-  };
   auto mask = [&](int s, floatx16 (&sc)[R]) {
     if (!masked(s)) return;
 #pragma unroll
@@ -206,7 +197,6 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
     // sets of registers), the requests spread over the steps (all at once they hold up the wave that makes them).
     auto step = [&](const floatx16 (&from)[R], floatx16 (&to)[R], bool masks) {  // from: the scores of stage s, to: those of stage s + 1
       ready();
-      if (masks) look(s);
       int64_t off[KW][F::kParts];
       uint32_t dst[KW];
 #pragma unroll
@@ -248,7 +238,6 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
 #pragma unroll
       for (int t = 0; t < R; t++) sc[t] = sd[t];
     }
-    look(s);
 #pragma unroll
     for (int t = 0; t < R; t++) probs<D, false>(sc[t], st[t], c2, pb[t]);
     add_unit();
@@ -314,15 +303,13 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
     int s = 0;
     for (; s + 1 < nst; s++) {
       ready();
-      look(s);
       feed.request_units(KW);
       advance();
     }
-    look(s);
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
   if (CARE) __syncthreads();  // every wave is done with the ring
-  else if (any_odd<D>(st, odd, odd_waves, w, l)) return true;
+  else if (any_odd<D>(st, odd, w, l)) return true;
   // With two key groups each finishes one half of the pieces: all park their accumulators and (mref, l) in the
   // ring, then each adds up the groups' for its own pieces.
   constexpr int P = Part::P, PP = P / KW;
@@ -366,10 +353,10 @@ __device__ __forceinline__ bool sweep_few(const AttnParams& p, const TileJob& jb
 }
 
 // Tiles of up to 256 rows in long sweeps, four wavefronts of two row tiles, one workgroup to a compute unit: an operand read from LDS serves 64
-// rows.  Units that some query does not see whole, few there, are taken one at a time and with care in any case.  Without CARE it returns
-// true where all units have to be.
+// rows.  Units that some query does not see whole, few there, are taken one at a time and with care in any case (without, the compiler moves the sums
+// between register files in the other units' loop: 4096 tokens behind 28672 2170 us, and 1820).  Without CARE it returns true where all units have to be.
 template <int D, bool PG, bool CARE>
-__device__ __forceinline__ bool sweep_tall(const AttnParams& p, const TileJob& jb, TileLds& sh, int (&odd_waves)[kWideWaves], uint4* ring) {
+__device__ __forceinline__ bool sweep_tall(const AttnParams& p, const TileJob& jb, TileLds& sh, int (&odd)[kWideWaves], uint4* ring) {
   constexpr int R = 2;
   using Part = PartialLayout<D, 32, true>;
   using F = Feed<D, kWideWaves, 32>;
@@ -470,8 +457,7 @@ __device__ __forceinline__ bool sweep_tall(const AttnParams& p, const TileJob& j
   auto add_unit = [&](int s, const bf16x8 (&pb)[R][2], uint32_t place) {
     const uint32_t va = lane_v + place;
     const bool careful = CARE || k0 + s * kUnitKeys + kUnitKeys > S;  // (uniform)
-    bool odd = false, odd_p = false;
-    // (the denominator's MFMA has the probabilities of two queries in a column, one of them times 0)
+    bool odd_v = false, odd_p = false;
 #pragma unroll
     for (int t = 0; t < R; t++)
 #pragma unroll
@@ -482,11 +468,11 @@ __device__ __forceinline__ bool sweep_tall(const AttnParams& p, const TileJob& j
 #pragma unroll
       for (int dt = 0; dt < D / 32; dt++) {
         bf16x8 a = read_v<D>(va, dt, j);
-        if (careful) a = finite_only(a, odd);
+        if (careful) a = finite_only(a, odd_v);
 #pragma unroll
         for (int t = 0; t < R; t++) st[t].o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t][j], st[t].o[dt], 0, 0, 0);
       }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd_v) != 0, 0)) {
 #pragma unroll
       for (int t = 0; t < R; t++) add_odd_values<D>(st[t].o, pb[t][0], pb[t][1], (uint32_t)(uintptr_t)(CB_LDS uint4*)ring + place + kSlotBytes / 2, (seen[t] < k1 ? seen[t] : k1) - k0 - s * kUnitKeys, l);
     }
@@ -570,7 +556,7 @@ __device__ __forceinline__ bool sweep_tall(const AttnParams& p, const TileJob& j
     for (; s + 1 < nst; s++) top();
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
-  if (!CARE && any_odd<D>(st, 0, odd_waves, w, l)) return true;
+  if (!CARE && any_odd<D>(st, odd, w, l)) return true;
 #pragma unroll
   for (int t = 0; t < R; t++) {
     floatx4 f[Part::P];
@@ -734,7 +720,6 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
     bare_barrier();
   };
   const int whole_end = S < k1 ? S : k1;
-  const bool hides = S < k1;  // (not for single tokens)
   auto masked = [&](int s) { return k0 + (s + 1) * kUnitKeys > whole_end; };
   const uint32_t ring = (uint32_t)(uintptr_t)(CB_LDS uint4*)sh.ring, vring = ring + L::kK * L::kBytes;
   const uint32_t lane_k = ring + lane_k_byte<D>(l), lane_v = vring + lane_v_byte<D>(l);
@@ -742,14 +727,6 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
   uint32_t k_at = 0, v_at = 0;  // places of the K that is read next and of V(s)
   auto advance_k = [&] { k_at = k_at + L::kBytes == L::kK * L::kBytes ? 0 : k_at + L::kBytes; };
   auto advance_v = [&] { v_at = v_at + L::kBytes == L::kV * L::kBytes ? 0 : v_at + L::kBytes; };
-  uint32_t odd = 0;  // bits 15 and 31: infinities or NaN
-  auto look = [&](int s) {  // the unit's values, this wavefront's share
-    if (!hides || !masked(s)) return;
-    constexpr uint32_t kShare = L::kBytes / kWideWaves;
-#pragma unroll
-    for (uint32_t x = 0; x < kShare; x += 1024) odd = odd_bits(__builtin_bit_cast(uintx4, *(const CB_LDS uintx4*)(vring + v_at + w * kShare + x + l * 16)), odd);
-    asm volatile("" : "+v"(odd));  // (the reads are through before the next barrier)
-  };
   auto mask = [&](int s, floatx16 (&sc)[R]) {
     if (!masked(s)) return;
 #pragma unroll
@@ -781,7 +758,6 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
     // A step: the scores of unit s + 1 beside the exponentials of unit s, then its values, beside which K of unit s + 2 is read.
     auto step = [&](int s, const floatx16 (&from)[R], floatx16 (&to)[R], bool masks) {  // from: the scores of unit s, to: those of unit s + 1
       ready();
-      if (masks) look(s);
       feed.next();
       score_half<D, false, R, F::kReq>(k, st, from, to, pw, lane_v + v_at, v, c2, [&](int i) { feed.request(i); });
       feed.requested(true, true);
@@ -802,7 +778,6 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
       for (int t = 0; t < R; t++) sc[t] = sd[t];
     }
     ready();
-    look(s);
     bf16x8 pb[R][2];
 #pragma unroll
     for (int t = 0; t < R; t++) {
@@ -863,15 +838,13 @@ __device__ __forceinline__ bool sweep_many(const AttnParams& p, const TileJob& j
   else {  // no rows of its own: it only brings its share, passing the same barriers
     for (int s = 0; s + 1 < nst; s++) {
       ready();
-      look(s);
       feed.request_step();
       advance_v();
     }
     ready();
-    look(nst - 1);
   }
   wait_vmcnt<0>();  // (the requests past the split's end, before the ring serves anything else)
-  if (!CARE && any_odd<D>(st, odd, sh.odd, w, l)) return true;
+  if (!CARE && any_odd<D>(st, sh.odd, w, l)) return true;
 #pragma unroll
   for (int t = 0; t < R; t++) {
     floatx4 f[Part::P];
@@ -915,8 +888,8 @@ __device__ __forceinline__ void merge_by_last(const AttnParams& p, const TileJob
     const int row = jb.row0 + i * 32 + (l & 31), token = row / jb.g;
     const int64_t gr = row < jb.M ? (int64_t)(jb.off + token) * p.Hq + jb.hk * jb.g + (row - token * jb.g) : -1;
     const uint32_t byte = partial_byte<D, 32, true>(p, jb, i);
-    if (flag == 1) merge_pieces<D, 32, true, P, 0, 2>(prsrc, gr, byte, (CB_GLOBAL uint16_t*)p.out, jb.nsplit, 0, l);
-    else merge_pieces<D, 32, true, P, kAgentCoherent, 2>(prsrc, gr, byte, (CB_GLOBAL uint16_t*)p.out, jb.nsplit, 0, l);
+    if (flag == 1) merge_pieces<D, 32, true, P, 0, 2, true>(prsrc, gr, byte, (CB_GLOBAL uint16_t*)p.out, jb.nsplit, 0, l);
+    else merge_pieces<D, 32, true, P, kAgentCoherent, 2, true>(prsrc, gr, byte, (CB_GLOBAL uint16_t*)p.out, jb.nsplit, 0, l);
   }
 }
 
@@ -932,7 +905,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_few(AttnParams p_a
   TileJob jb;
   if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
   if (sweep_few<D, PG, false>(p, jb, sh, odd, ring)) sweep_few<D, PG, true>(p, jb, sh, odd, ring);
-  if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
+  if (jb.nsplit > 1) split_merge<D, 32, true, kWideWaves, 128, false, true>(p, jb, p.tile_rows, sh, nullptr, [] {});
 }
 
 template <int D, bool PG>
@@ -948,7 +921,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 1) void k_chunk_tall(AttnParams p_
   if (!chunk_job(p, ml, lane_chunk, blockIdx.x, jb)) return;
   if (sweep_tall<D, PG, false>(p, jb, sh, odd, ring)) sweep_tall<D, PG, true>(p, jb, sh, odd, ring);
   if (jb.nsplit == 1) return;
-  if (p.coop_merge) split_merge<D, 32, true, kWideWaves, 256, false>(p, jb, p.tile_rows, sh, nullptr, [] {});
+  if (p.coop_merge) split_merge<D, 32, true, kWideWaves, 256, false, true>(p, jb, p.tile_rows, sh, nullptr, [] {});
   else merge_by_last<D>(p, jb, &sh.flag);
 }
 
@@ -969,7 +942,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void k_chunk_many(AttnParams p_
   }
   __syncthreads();  // (everybody is done with the rings, whose place the merge's words take)
   static_assert(sizeof(TileLds) <= sizeof(sh.ring), "");
-  split_merge<D, 32, true, kWideWaves, 128, false>(p, jb, p.tile_rows, *reinterpret_cast<TileLds*>(sh.ring), nullptr, [] {});
+  split_merge<D, 32, true, kWideWaves, 128, false, true>(p, jb, p.tile_rows, *reinterpret_cast<TileLds*>(sh.ring), nullptr, [] {});
 }
 
 int64_t chunk_partial_bytes(int D, int64_t total, int Hq, int Hkv, int batch) {

@@ -526,8 +526,9 @@ __device__ __forceinline__ void store_row(CB_GLOBAL uint16_t* gout, int64_t grow
 // combined online, BS per batch with all of a batch's loads in flight together: m = max m_t, w_t = 2^(m_t - m),
 // o = sum w_t o_t / sum w_t l_t (m_t is stored in log2 units).  POL is the buffer cache policy of
 // the loads.  A slot that saw no visible key carries m_t = -inf, l_t = 0 and gets weight 0; the
-// reference is kept finite so that (-inf) - (-inf) never occurs.  grow: the lane's output row, or -1.
-template <int D, int TR, bool PX, int NP, int POL, int BS>
+// reference is kept finite so that (-inf) - (-inf) never occurs.  grow: the lane's output row, or -1.  ODD: states may hold infinities, so a
+// batch's places behind the last slot are left out; otherwise they are added with weight 0.
+template <int D, int TR, bool PX, int NP, int POL, int BS, bool ODD = false>
 __device__ __forceinline__ void merge_pieces(__amdgpu_buffer_rsrc_t prsrc, int64_t grow, uint32_t byte, CB_GLOBAL uint16_t* gout,
                                              int nslots, int pc0, int l) {
   using Part = PartialLayout<D, TR, PX>;
@@ -566,6 +567,7 @@ __device__ __forceinline__ void merge_pieces(__amdgpu_buffer_rsrc_t prsrc, int64
     m_run = m_new;
 #pragma unroll
     for (int u = 0; u < BS; u++) {
+      if (ODD && t0 + u >= nslots) break;  // (uniform)
       float wgt = __builtin_amdgcn_exp2f(__uint_as_float(ml[u][0]) - m_new);
       wgt = (t0 + u < nslots) ? wgt : 0.f;
       lsum = fmaf(__uint_as_float(ml[u][1]), wgt, lsum);
@@ -597,8 +599,8 @@ __device__ __forceinline__ void merge_pieces(__amdgpu_buffer_rsrc_t prsrc, int64
 // sum = n*id and sumsq = n*id*id.  A second word per tile holds one bit per split whose
 // workgroup gave up waiting (cooperative merge only).
 // aside(): what the first wave has to do beside, where it would wait for the other splits, or, in the merge by the last to arrive, behind its
-// share of that.
-template <int D, int TR, bool PX, int NW, int MAXROWS, bool TS, typename Aside>
+// share of that.  ODD: see merge_pieces.
+template <int D, int TR, bool PX, int NW, int MAXROWS, bool TS, bool ODD = false, typename Aside>
 __device__ __forceinline__ void split_merge(const AttnParams& p, const TileJob& jb, int tile_rows, TileLds& sh, CB_LDS unsigned long long* ts, Aside aside) {
   constexpr int P = PartialLayout<D, TR, PX>::P;
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
@@ -657,8 +659,8 @@ __device__ __forceinline__ void split_merge(const AttnParams& p, const TileJob& 
       int64_t gr;
       if (!tile_row(i, &gr)) break;  // (nothing behind it either)
       const uint32_t byte = partial_byte<D, TR, PX>(p, jb, i);
-      if (flag == 1) merge_pieces<D, TR, PX, NP, 0, BS>(prsrc, gr, byte, gout, nsplit, (u % (P / NP)) * NP, l);
-      else merge_pieces<D, TR, PX, NP, kAgentCoherent, BS>(prsrc, gr, byte, gout, nsplit, (u % (P / NP)) * NP, l);
+      if (flag == 1) merge_pieces<D, TR, PX, NP, 0, BS, ODD>(prsrc, gr, byte, gout, nsplit, (u % (P / NP)) * NP, l);
+      else merge_pieces<D, TR, PX, NP, kAgentCoherent, BS, ODD>(prsrc, gr, byte, gout, nsplit, (u % (P / NP)) * NP, l);
     }
     if (w == 0) aside();
     if (!flag) return;
@@ -733,8 +735,8 @@ __device__ __forceinline__ void split_merge(const AttnParams& p, const TileJob& 
     const int pc = u % upt * np;
     auto go = [&](auto n, auto bs) {
       constexpr int NP = decltype(n)::value, BS = decltype(bs)::value;
-      if (flag == 1) merge_pieces<D, TR, PX, NP, 0, BS>(prsrc, gr, byte, gout, nsplit, pc, l);
-      else merge_pieces<D, TR, PX, NP, kAgentCoherent, BS>(prsrc, gr, byte, gout, nsplit, pc, l);
+      if (flag == 1) merge_pieces<D, TR, PX, NP, 0, BS, ODD>(prsrc, gr, byte, gout, nsplit, pc, l);
+      else merge_pieces<D, TR, PX, NP, kAgentCoherent, BS, ODD>(prsrc, gr, byte, gout, nsplit, pc, l);
     };
     using std::integral_constant;
     constexpr int LONG = PX && !SMALL ? 8 : 16;  // (as many loads as the registers hold)

@@ -81,3 +81,24 @@ def test_values_come_through_whatever_their_weight(dtype, d, rows, splits):
     for what in WHAT:
         for t in (0, 20, 59):
             assert not _spoil_value(b, 70 + t, t, what).isfinite().any(), (what, t)
+
+
+@pytest.mark.parametrize("dtype, d, rows", TILES)
+@pytest.mark.parametrize("kv_len, new, splits, slot", [(40, 1, 1, 40), (95, 1, 1, 95), (700, 1, 0, 700), (287, 1, 3, 95), (1000, 2, 2, 511), (70, 60, 3, 33)])
+def test_the_last_value_of_a_split_comes_through(dtype, d, rows, kv_len, new, splits, slot):
+    """The places behind a split's last key repeat it, with weight 0."""
+    print(f"[case] odd last value {dtype} {d} {rows} {kv_len}+{new} {splits} {slot}", flush=True)
+    b = Batch(dtype, 8, 2, d, [kv_len], [new], 16, seed=8)
+    _options(b, rows, splits)
+    b.v = b.v.view(-1, b.hkv, d)  # (a slot of the cache is a row)
+    at = int(b.table[0, slot // 16]) * 16 + slot % 16
+    import torch
+    clean, kept = _attend(b), b.v[at, 1, 5].clone()
+    for what in WHAT:
+        b.v[at, 1, 5] = what
+        got = _attend(b)
+        mine = got[max(0, slot - kv_len):, 4:8, 5]
+        assert (mine.isnan() if what != what else mine == what).all(), what
+        mine.copy_(clean[max(0, slot - kv_len):, 4:8, 5])
+        assert torch.equal(got, clean), what
+    b.v[at, 1, 5] = kept
