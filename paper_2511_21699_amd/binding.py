@@ -353,7 +353,7 @@ class Verifier:
 
     # ---- around the verification: tokens into the cache, their attention, their probabilities.  The `bind_` forms marshal once and return a
     # zero-argument callable that only makes the C call; it reads the int32 arrays kv_len and token_offsets that it was given anew in every call,
-    # so a loop changes them in place.
+    # so a loop changes them in place; token_offsets that outgrow the tensors are refused, as the C call does not know their sizes.
     def bind_append_kv(self, q, k, v, prep: CbHeadPrep, kv: CbKvLayer, kv_len, token_offsets, q_out, d_parent=None, stream=None):
         """Pre-marshalled cb_append_kv_device.  q [n, Hq, D], k and v [n, Hkv, D] can be views of one product's rows; q and q_out may both
         be None.  prep.q_weight and prep.k_weight must have head_dim entries."""
@@ -372,7 +372,8 @@ class Verifier:
         at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         a = (self.ctx, self._stream(stream), len(kv_len), at(q), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2], C.byref(prep), C.byref(kv),
              _ip(kv_len), _ip(token_offsets), at(d_parent), at(q_out))
-        return self._bound(self._F.cb_append_kv_device, a, (kv_len, token_offsets, q, k, v, prep, kv, d_parent, q_out))
+        room = min([t.shape[0] for t in (q, k, v, q_out) if t is not None] + [d_parent.numel() if d_parent is not None else k.shape[0]])
+        return self._bound(self._F.cb_append_kv_device, a, (kv_len, token_offsets, q, k, v, prep, kv, d_parent, q_out), token_offsets, room)
 
     def append_kv(self, q, k, v, prep: CbHeadPrep, kv: CbKvLayer, kv_len, token_offsets, q_out, d_parent=None, stream=None):
         """Normalise and rotate new tokens' query and key heads and put their K/V into the cache (cb_append_kv_device)."""
@@ -385,7 +386,7 @@ class Verifier:
         for name, t in (("q", q), ("attn_out", attn_out)):
             self._heads(name, t, n, self.cfg.num_q_heads, True)
         a = (self.ctx, self._stream(stream), len(kv_len), q.data_ptr(), C.byref(kv), _ip(kv_len), _ip(token_offsets), attn_out.data_ptr())
-        return self._bound(self._F.cb_chunk_attention_device, a, (kv_len, token_offsets, q, kv, attn_out))
+        return self._bound(self._F.cb_chunk_attention_device, a, (kv_len, token_offsets, q, kv, attn_out), token_offsets, min(q.shape[0], attn_out.shape[0]))
 
     def chunk_attention(self, q, kv: CbKvLayer, kv_len, token_offsets, attn_out=None, stream=None):
         """Attention of new tokens over the cache that holds their K/V already (cb_chunk_attention_device); returns attn_out."""
@@ -418,8 +419,10 @@ class Verifier:
         self.bind_token_logprobs(logits, d_tokens, top_k, *out, d_rows=d_rows, stream=stream)()
         return out
 
-    def _bound(self, fn, a, keep):
+    def _bound(self, fn, a, keep, offsets=None, room: int = 0):
         def call(_keep=(self, keep)):
+            if offsets is not None and offsets[-1] > room:
+                raise ValueError(f"token_offsets ends at {offsets[-1]}, the tensors bound hold {room} tokens")
             rc = fn(*a)
             if rc:
                 self._raise(rc)
