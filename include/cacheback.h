@@ -307,7 +307,8 @@ int cb_token_logprobs_device(cb_ctx *ctx, void *hip_stream, const void *logits, 
                              float *d_logprob, float *d_entropy, int32_t top_k, int32_t *d_top_tokens,
                              float *d_top_logprobs);
 
-/* Test hooks (each synchronises the stream of the last verify call).
+/* Test hooks (each synchronises the stream of the last verify call; cb_device_status that of the last call around the verification too,
+ * which has to exist still.  For graphs replayed on other streams the caller waits first; a bit that is set later is kept for the next reading).
  *   cb_get_path     host [batch][max_depth+1]: node indices of the accepted path, -1 padded
  *   cb_get_argmax   host [sumN]: first-maximum index of each logits row
  *   cb_device_status  0, or a bit mask: 1 = malformed parent entry seen, 2 = node deeper than max_depth,

@@ -85,7 +85,7 @@ WsLayout ws_layout(const cb_config& c) {
   L.res_tok = L.res_len;                              // (placed per call)
   L.new_len = take(c.max_batch * 4);
   // from here to the timing table: the words that start at zero, cleared together by cb_init
-  L.status = take(4);
+  L.status = take(8);  // (and what cb_device_status takes out of it)
   L.tickets = take((size_t)L.ticket_count * 4);
   L.coop_tickets = take((size_t)kCoopTiles * kCoopTicketStride);
   L.amax_tickets = take((size_t)c.max_batch * kTicketWords * 4);
@@ -145,6 +145,8 @@ struct cb_ctx {
   int32_t call_seq = 0;        // sequence number of the last host-form call (never 0 once used)
   int32_t* want_done = nullptr;  // these two are set by cb_verify_tree for the launch it is about to make
   int32_t* want_last = nullptr;
+  hipStream_t beside = nullptr;  // stream of the last call around the verification, unless the status has been read since
+  bool have_beside = false;
   hipStream_t unsynced = nullptr;  // stream that may still run the tail of a host-form call that has returned
   bool have_unsynced = false;
   int32_t* d_hblock = nullptr;  // the pinned block's address on the device
@@ -1223,6 +1225,8 @@ int before_launch(cb_ctx* ctx, hipStream_t st) {
   int device = -1;
   CB_HIP(ctx, hipGetDevice(&device));
   if (device != ctx->device) return set_err(ctx, CB_EINVAL, "the context is of device %d, the current one is %d", ctx->device, device);
+  ctx->beside = st;
+  ctx->have_beside = true;
   return order_behind_host_form(ctx, st);
 }
 
@@ -1939,11 +1943,14 @@ int cb_get_argmax(cb_ctx* ctx, int32_t* argmax) {
 int cb_device_status(cb_ctx* ctx, int32_t* status) {
   if (!ctx || !status) return set_err(ctx, CB_EINVAL, "null argument");
   hipStream_t st = ctx->have_verify ? ctx->last_stream : nullptr;
-  CB_HIP(ctx, hipMemcpyAsync(ctx->h_misc, ctx->dev<int32_t>(ctx->lay.status), 4, hipMemcpyDeviceToHost, st));
+  if (ctx->have_beside && ctx->beside != st) CB_HIP(ctx, hipStreamSynchronize(ctx->beside));
+  ctx->have_beside = false;
+  // Reading clears the sticky word, in one step: what a launch sets meanwhile is there at the next reading.
+  int32_t* const word = ctx->dev<int32_t>(ctx->lay.status);
+  CB_HIP(ctx, launch_take_word(st, word, word + 1));
+  CB_HIP(ctx, hipMemcpyAsync(ctx->h_misc, word + 1, 4, hipMemcpyDeviceToHost, st));
   CB_HIP(ctx, hipStreamSynchronize(st));
   *status = ctx->h_misc[0];
-  CB_HIP(ctx, hipMemsetAsync(ctx->dev<int32_t>(ctx->lay.status), 0, 4, st));  // reading clears the sticky word
-  CB_HIP(ctx, hipStreamSynchronize(st));
   return CB_OK;
 }
 

@@ -230,6 +230,7 @@ hipError_t launch_tree_prepare(hipStream_t st, int batch, const SeqMeta& meta, c
                                int max_depth, uint32_t* anc, int32_t* status);
 // zeroes `run` 64-bit words at each of `count` places `stride` words apart
 hipError_t launch_zero_words(hipStream_t st, unsigned long long* base, int count, int stride, int run);
+hipError_t launch_take_word(hipStream_t st, int32_t* word, int32_t* taken);  // *taken = *word, *word = 0
 struct AcceptArgs;  // cb_logits.h
 struct LogitsWork;
 // scans the logits and, with lw.accept_after, runs the acceptance (lw.n_wgs is chosen here); with prep_parent !=

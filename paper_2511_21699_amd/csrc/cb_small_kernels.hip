@@ -70,6 +70,12 @@ hipError_t launch_zero_words(hipStream_t st, unsigned long long* base, int count
   return hipGetLastError();
 }
 
+__global__ void k_take_word(int32_t* word, int32_t* taken) { *taken = __hip_atomic_exchange(word, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+hipError_t launch_take_word(hipStream_t st, int32_t* word, int32_t* taken) {
+  hipLaunchKernelGGL(k_take_word, dim3(1), dim3(1), 0, st, word, taken);
+  return hipGetLastError();
+}
+
 hipError_t launch_tree_prepare(hipStream_t st, int batch, const SeqMeta& meta, const int32_t* parent,
                                int max_depth, uint32_t* anc, int32_t* status) {
   hipLaunchKernelGGL(k_tree_prepare, dim3(batch), dim3(256), 0, st, meta, parent, max_depth, anc, status);
