@@ -1124,7 +1124,7 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     double dim64;                            // alone and full at head_dim 64
   };
   // From launches of 1 to 8192 tokens of 32/8 and 32/32 heads over up to 65536 keys.  With tiles of 64, 128 and 256 rows 8192 tokens from the first take
-  // 726, 533 and 516 us, 4096 behind 28672 3059, 2102 and 1821, 256 behind 30000 in one split 382, 569 and 792, in eight 240, 156 and 131.
+  // 738, 506 and 540 us, 4096 behind 28672 3052, 1984 and 1785, 256 behind 30000 in one split 377, 568 and 789, in eight 228, 158 and 145.
   static const Tile kBf16[] = {{64, 0.36, 0.36, 5.5, 2.0, 4.0, 0.78}, {128, 0.66, 0.52, 4.5, 3.2, 5.0, 0.7}, {256, 0.86, 0.96, 8.0, 4.0, 10.0, 1.0}};
   static const Tile kF32[] = {{16, 0.75, 0.75, 6.0, 1.0, 6.0, 0.6}, {32, 1.4, 1.4, 8.0, 1.0, 6.0, 0.6}};
   ChunkPlan best{};
@@ -1144,7 +1144,7 @@ ChunkPlan plan_chunk(const cb_config& c, const WsLayout& lay, int opt_splits, in
     if (tiles > 0 && tiles <= 1024 && (int64_t)batch * Hkv * tiles_max <= tickets)
       most = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(lay.total - lay.partial) / per_split, most_here, lay.max_splits, (len_max + 63) / 64, 1024}));
     // Splits of the longest sequence, in tenths: 1.2 and 1.5 cut only the longest of tiles that differ in length (a prompt of 2048, 32/32 heads, in one
-    // split 55.8 us, in 1.2 53.8, in two 60; of 1024 28.1, 24.2 and 26.5).
+    // split 49.1 us, in 1.2 48.6, in two 59.8; of 1024 26.4, 22.6 and 24.1).
     auto next = [](int t) { return t < 12 ? 12 : t < 15 ? 15 : t < 20 ? 20 : t + 10 + t / 120 * 10; };
     int tenths = opt_splits > 0 ? 10 * std::min(opt_splits, most) : 10;
     for (int last = 0;; tenths = next(tenths)) {

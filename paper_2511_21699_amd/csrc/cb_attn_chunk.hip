@@ -7,9 +7,9 @@
 // Probabilities are rounded to bf16, the matrix cores' type (half a step each, in the numerator and, the same, in the denominator); sums,
 // statistics and partial states are in 32 bits.
 //
-// What bounds it, at 32/8 heads of 128: long sweeps the matrix cores beside the vector units, together all of a compute unit's time, at the 1.8 GHz that
-// this power allows (4096 tokens behind 28672 1.85 ms, 1110 TFLOP/s; the products alone 1250); single tokens reading the cache (16
-// sequences of up to 16384 105 us, 5.0 TB/s); short chunks a launch, a workgroup's start and the way of a split's state through memory (1024 tokens from
+// What bounds it, at 32/8 heads of 128: long sweeps the matrix cores beside the vector units, at the 1.9 to 2.1 GHz that this power allows (4096 tokens
+// behind 28672 1.82 ms, 1130 TFLOP/s; a library product's rate is 1250; a compute unit's matrix cores are busy 56% of its time, its vector units 47%, both
+// 24%); single tokens reading the cache (16 sequences of up to 16384 105 us, 5.0 TB/s); short chunks a launch, a workgroup's start and the way of a split's state through memory (1024 tokens from
 // the first 24 us).  Hence three tiles, for a rule by the host: of 64 rows, whose workgroup has the whole ring of LDS for keys on their way, of
 // 128, two to a compute unit, and of 256, which read an operand from LDS for 64 rows.
 #include "cb_attn_wide.h"

@@ -6,8 +6,8 @@
 // A workgroup of 8 wavefronts has RT row tiles of 16 rows of a kv head and a split of their keys.  The wavefronts take units of 16 keys in turn
 // and share nothing until the end: K and V go straight from memory to the registers that the MFMAs read, and serve RT tiles.  The
 // wavefronts' states are combined through LDS, the splits' by the tile's last workgroup.
-// What bounds it: prompts the matrix cores, a unit is RT D / 2 MFMAs of 32 cycles with two wavefronts to a SIMD (heads of 128, two row tiles: busy 63%
-// of the time at 2.16 GHz, waiting for V most of the rest; 32/8 heads, 512 tokens behind 4096 in 380 us, 96 TFLOP/s).  Single tokens the loads on their way:
+// What bounds it: prompts the matrix cores, a unit is RT D / 2 MFMAs of 32 cycles with two wavefronts to a SIMD (heads of 128, two row tiles: busy 62%
+// of the launch at 2.19 GHz, the wavefronts waiting 62% of theirs; 32/8 heads, 512 tokens behind 4096 in 372 us, 98 TFLOP/s).  Single tokens the loads on their way:
 // a compute unit takes 39 bytes a ns.  One token behind 8192 25 us, 16 behind 2000 each 57 us (4.6 TB/s); with a table's entries asked for
 // where they are needed, V not ahead and eight splits at a time in the merge these were 40 and 78.
 //

@@ -4,7 +4,7 @@
 // pass with the running maximum m; everything in 32 bits.  A wavefront takes 64 keys at a time: a lane scores one, then owns D / 64 dims
 // of the sum.  It takes every shape, at the pace of the plain arithmetic and with K and V read once per row: for blocks of a size that is no
 // power of two in bf16, whose keys the matrix-core kernels' loads could not place with shifts, and to compare with.  2048 tokens of 32/32
-// heads of 128 behind nothing take 3.0 ms, on the matrix cores 55 us.
+// heads of 128 behind nothing, in blocks of 24, take 2.8 ms; on the matrix cores, in blocks of 32, 52 us.
 #include "cb_internal.h"
 
 namespace cb {
