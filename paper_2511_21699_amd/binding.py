@@ -367,6 +367,7 @@ class Verifier:
             t = getattr(prep, "_keep", (None, None, None))[name == "k_weight"]
             if w and t is not None and t.numel() != cfg.head_dim:
                 raise ValueError(f"{name} must have head_dim entries")
+        self._here(**dict(zip(("q_weight", "k_weight", "inv_freq"), getattr(prep, "_keep", ()))), d_parent=d_parent)
         if d_parent is not None and (str(d_parent.dtype) != "torch.int32" or not d_parent.is_contiguous() or d_parent.numel() < n):
             raise ValueError("d_parent must be a contiguous int32 tensor of one entry per token")
         at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
@@ -405,6 +406,7 @@ class Verifier:
                                    ("top_tokens", top_tokens, "int32", n * top_k), ("top_logprobs", top_logprobs, "float32", n * top_k)):
             if t is not None and (str(t.dtype) != "torch." + dt or not t.is_contiguous() or t.numel() != count):
                 raise ValueError(f"{name} must be a contiguous {dt} tensor of {count} entries")
+        self._here(logits=logits, d_rows=d_rows, d_tokens=d_tokens, logprob=logprob, entropy=entropy, top_tokens=top_tokens, top_logprobs=top_logprobs)
         at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         a = (self.ctx, self._stream(stream), logits.data_ptr(), max(logits.stride(0), cfg.vocab_size) if logits.shape[0] <= 1 else logits.stride(0), logits.shape[0], n, at(d_rows),
              at(d_tokens), at(logprob), at(entropy), top_k, at(top_tokens) if top_k else None, at(top_logprobs) if top_k else None)
@@ -434,6 +436,12 @@ class Verifier:
             raise ValueError(f"{name} must have one entry more than kv_len")
         return int(offsets[-1])
 
+    def _here(self, **tensors):
+        """Kernels take addresses: a tensor of another device has none that they could use."""
+        for name, t in tensors.items():
+            if t is not None and t.device != self.workspace.device:
+                raise ValueError(f"{name} is on {t.device}, the context on {self.workspace.device}")
+
     def _heads(self, name: str, t, n: int, heads: int, contiguous: bool = False) -> int:
         """The token stride of a [>= n, heads, head_dim] tensor of the configuration's type."""
         if t is None and name == "q":
@@ -441,6 +449,7 @@ class Verifier:
         d, want = self.cfg.head_dim, "torch.float32" if self.cfg.qkv_dtype == CB_F32 else "torch.bfloat16"
         if t.dim() != 3 or t.shape[0] < n or tuple(t.shape[1:]) != (heads, d) or str(t.dtype) != want or t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
             raise ValueError(f"{name} must be [>= {n}, {heads}, {d}] in {want} with a token's heads side by side")
+        self._here(**{name: t})
         if contiguous and t.shape[0] > 1 and t.stride(0) != heads * d:
             raise ValueError(f"{name} must be contiguous")
         return max(t.stride(0), heads * d) if t.shape[0] <= 1 else t.stride(0)

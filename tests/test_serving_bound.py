@@ -20,6 +20,8 @@ class _Calls:
 
 def _verifier(hq=4, hkv=2, d=64):
     v = object.__new__(B.Verifier)
+    import torch
+    v.workspace = torch.zeros(1)
     v.cfg, v.ctx, v._F, v._stream = B.make_config(hq, hkv, d, "f32", "f32", 2, 16, 4, 20), None, _Calls(), lambda stream: None
     return v
 
@@ -58,3 +60,35 @@ def test_offsets_that_outgrow_the_tensors_are_refused(which, short):
             call()
     off[2] = 5
     call()
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "out", "parent", "q_weight", "k_weight", "inv_freq"])
+def test_tensors_of_another_device_are_refused(which):
+    """(Here the context's device is the CPU; a kernel would be given an address of the other one.)"""
+    import torch
+    place = lambda name, t: t.to("meta") if name == which else t  # noqa: E731
+    ver = _verifier()
+    q, out = place("q", torch.zeros(5, 4, 64)), place("out", torch.zeros(5, 4, 64))
+    k, v, parent = place("k", torch.zeros(5, 2, 64)), place("v", torch.zeros(5, 2, 64)), place("parent", torch.zeros(5, dtype=torch.int32))
+    prep = B.head_prep(place("q_weight", torch.ones(64)), place("k_weight", torch.ones(64)), 1e-6, place("inv_freq", torch.ones(16)))
+    with pytest.raises(ValueError, match=which + ".*meta"):
+        ver.bind_append_kv(q, k, v, prep, B.CbKvLayer(), [3], [0, 5], out, d_parent=parent)
+    if which in ("q", "out"):
+        with pytest.raises(ValueError, match=which + ".*meta"):
+            ver.bind_chunk_attention(q, B.CbKvLayer(), [3], [0, 5], out)
+
+
+@pytest.mark.parametrize("which", ["logits", "d_rows", "d_tokens", "logprob", "entropy", "top_tokens", "top_logprobs"])
+def test_logits_of_another_device_are_refused(which):
+    import torch
+    ver = _verifier()
+    ver._F.cb_token_logprobs_device = ver._F._call
+    t = dict(logits=torch.zeros(3, 20), d_rows=torch.zeros(3, dtype=torch.int32), d_tokens=torch.zeros(3, dtype=torch.int32), logprob=torch.zeros(3), entropy=torch.zeros(3),
+             top_tokens=torch.zeros(3, 2, dtype=torch.int32), top_logprobs=torch.zeros(3, 2))
+
+    def bind():
+        return ver.bind_token_logprobs(t["logits"], t["d_tokens"], 2, t["logprob"], t["entropy"], t["top_tokens"], t["top_logprobs"], d_rows=t["d_rows"])
+    bind()()
+    t[which] = t[which].to("meta")
+    with pytest.raises(ValueError, match=which + ".*meta"):
+        bind()
