@@ -1230,6 +1230,19 @@ int before_launch(cb_ctx* ctx, hipStream_t st) {
   return order_behind_host_form(ctx, st);
 }
 
+// The status word, which reading clears, in one step: what a launch sets meanwhile is there at the next reading.
+int take_status(cb_ctx* ctx, int32_t* status) {
+  hipStream_t st = ctx->have_verify ? ctx->last_stream : nullptr;
+  if (ctx->have_beside && ctx->beside != st) CB_HIP(ctx, hipStreamSynchronize(ctx->beside));
+  ctx->have_beside = false;
+  int32_t* const word = ctx->dev<int32_t>(ctx->lay.status);
+  CB_HIP(ctx, launch_take_word(st, word, word + 1));
+  CB_HIP(ctx, hipMemcpyAsync(ctx->h_misc, word + 1, 4, hipMemcpyDeviceToHost, st));
+  CB_HIP(ctx, hipStreamSynchronize(st));
+  *status = ctx->h_misc[0];
+  return CB_OK;
+}
+
 // The arguments of cb_append_kv_device, and what its kernel gets.
 int check_append(cb_ctx* ctx, int32_t batch, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                  const cb_head_prep* prep, const cb_kv_layer* kv, const int32_t* kv_len, const int32_t* token_offsets, const int32_t* d_tree_parent, void* q_out, AppendArgs* args, SeqMeta* meta) {
@@ -1942,16 +1955,13 @@ int cb_get_argmax(cb_ctx* ctx, int32_t* argmax) {
 
 int cb_device_status(cb_ctx* ctx, int32_t* status) {
   if (!ctx || !status) return set_err(ctx, CB_EINVAL, "null argument");
-  hipStream_t st = ctx->have_verify ? ctx->last_stream : nullptr;
-  if (ctx->have_beside && ctx->beside != st) CB_HIP(ctx, hipStreamSynchronize(ctx->beside));
-  ctx->have_beside = false;
-  // Reading clears the sticky word, in one step: what a launch sets meanwhile is there at the next reading.
-  int32_t* const word = ctx->dev<int32_t>(ctx->lay.status);
-  CB_HIP(ctx, launch_take_word(st, word, word + 1));
-  CB_HIP(ctx, hipMemcpyAsync(ctx->h_misc, word + 1, 4, hipMemcpyDeviceToHost, st));
-  CB_HIP(ctx, hipStreamSynchronize(st));
-  *status = ctx->h_misc[0];
-  return CB_OK;
+  int device = -1;  // (the null stream and the launch are to be those of the context's device, whichever is the current one)
+  CB_HIP(ctx, hipGetDevice(&device));
+  if (device == ctx->device) return take_status(ctx, status);
+  CB_HIP(ctx, hipSetDevice(ctx->device));
+  const int rc = take_status(ctx, status);
+  CB_HIP(ctx, hipSetDevice(device));
+  return rc;
 }
 
 int cb_set_option(cb_ctx* ctx, const char* name, int64_t value) {
